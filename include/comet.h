@@ -199,6 +199,95 @@ int comet_controller_tick(comet_controller *c, int *collect);
  * (all finite and > 0, else COMET_ERR_INVALID). */
 int comet_controller_update(comet_controller *c, const float *eb_old, const float *eb_new, uint32_t n_layers);
 
+/* ---- keys and values of attention layers ------------------------------------------------------
+ * What an attention layer keeps from one token to the next is activations as well, the ones a language model holds longest.
+ * A whole tensor's Huffman stream can neither grow by a token nor be read in place, so they have a form of their own: blocks
+ * of 32 tokens of one key/value head, uniformly quantised to 8 bits against the block's largest value, one scale for the
+ * keys and one for the values: |x - xhat| <= scale / 2 with scale = max(largest |x| / 127, 2^-100), up to float32 rounding.  The block a sequence
+ * is still filling lies in 16 bits, so every block is quantised once and the cache holds the same bytes whether the
+ * tokens came one by one or all at once.
+ *
+ * The cache is one device buffer of comet_cache_bytes(shape), 16-byte aligned, owned by the caller; its contents need no
+ * initialisation.  n_pages pages of page_tokens tokens (a multiple of 32) for each of `heads` heads of `dim` values (a multiple
+ * of 32 up to 256); n_slots sequences can have an open block.  Sections, for per = page_tokens / 32:
+ *   blocks  [n_pages][heads][per][64*dim]  keys int8 [dim/32][token][32], then values int8 [dim][place of the token]
+ *   scales  [n_pages][heads][per][2] float32: keys, values (the section is padded to a multiple of 256 bytes)
+ *   open    [n_slots][heads][2][128*dim + 256]  float16 in the same orders, then 32 float32 scales of the keys' tokens and 32 of
+ *           the values'; block j of a sequence is in half j % 2
+ * Token 16u + 8w + 4h + i of a block has place 16h + 8u + 4w + i.
+ *
+ * A batch describes, on the device, which tokens of which sequences a call is about; all three calls of a step take the same:
+ *   dev_starts  int32[n_seqs + 1]: sequence b's new tokens are rows starts[b] .. starts[b+1]-1 of the tensors passed with
+ *               it (none is fine; rows behind starts[n_seqs] are neither read nor written)
+ *   dev_lens    int32[n_seqs]: tokens sequence b holds once these are in: the new tokens have the places lens[b] - n .. lens[b] - 1
+ *   dev_table   int32[n_seqs][table_width]: the page of the tokens p * page_tokens ..; entries that are not reached are not read
+ *   dev_slots   int32[n_seqs], or NULL for slot b
+ * Two sequences of one append must not share a slot or a page that the call completes a block in (values undefined, never out of
+ * bounds).  Complete blocks are never written again by tokens that follow, so sequences may share the pages of a
+ * common beginning that ends with a block.  A sequence's length may be set back by up to 32 tokens (drafted tokens that are
+ * not taken): the slot keeps the open block and the one before it.
+ * Conditions known on the device only (rows outside the tensors, a page that is none, a slot that is none, lens[b] < n in an append or fetch) store
+ * COMET_ERR_FORMAT in *dev_status if that is given, and leave it alone otherwise (the caller clears it); what they
+ * touch is skipped: rows left as they were, tokens of a page that is none not seen.  A token whose key (value) holds Inf or NaN makes NaN of
+ * the keys (values) of its block and head when read back, and of the rows that see any of the block.
+ *
+ * Tensors are [tokens][heads][dim] with strides in elements; the dim values of a row are contiguous.  dtype: COMET_F16 or COMET_BF16
+ * (comet_rope: COMET_F32 too).  Everything is asynchronous on `stream` and may be captured into a HIP graph; a replay
+ * goes by what the batch's arrays hold then.  Nothing is allocated. */
+#define COMET_F32 0
+#define COMET_CACHE_BLOCK 32u
+typedef struct { uint32_t n_pages, page_tokens, n_slots, heads, dim; } comet_cache_shape;
+typedef struct { uint32_t n_seqs, table_width; const int32_t *dev_starts, *dev_lens, *dev_table, *dev_slots; } comet_cache_batch;
+typedef struct { void *dev; int64_t token_stride, head_stride; } comet_rows;
+
+/* Rotary positions: pair i of the first `rot` values of a head is turned by position * steps[i] turns and multiplied with amp;
+ * the values behind are left alone.  layout: COMET_ROPE_HALVES pairs (i, i + rot/2), COMET_ROPE_PAIRS (2i, 2i + 1).
+ * dev_steps: uint64[rot/2], turns per position in units of 2^-64, device memory of the caller: positions and steps are multiplied
+ * exactly, so angles are right to 2^-31 turns at any position below 2^31. */
+#define COMET_ROPE_HALVES 0u
+#define COMET_ROPE_PAIRS 1u
+typedef struct { uint32_t rot, layout; float amp; const uint64_t *dev_steps; } comet_rope_plan;
+
+/* The steps of a plan, on the host.  Frequencies base^(-2i/rot) radians per position (rot even, 2 .. 4096; base > 1), scaled for contexts `factor`
+ * (>= 1) times as long as the original_len tokens of the training: not at all; every frequency divided by the factor; the base raised to
+ * base * factor^(rot/(rot-2)); or by parts (arXiv 2309.00071): those of less than beta_slow turns in original_len divided, of more than
+ * beta_fast kept, in between in proportion, and *amp = 0.1 ln(factor) + 1 (1 otherwise).  beta_fast > beta_slow >= 0; original_len > 0. */
+#define COMET_ROPE_PLAIN 0u
+#define COMET_ROPE_LINEAR 1u
+#define COMET_ROPE_BASE 2u
+#define COMET_ROPE_PARTS 3u
+typedef struct { uint32_t rot, scaling; double base, factor, original_len, beta_fast, beta_slow; } comet_rope_cfg;
+int comet_rope_steps(const comet_rope_cfg *cfg, uint64_t *host_steps, float *amp);
+
+/* y = x turned by its tokens' positions (dev_positions: int32[n_tokens], or NULL for 0, 1, ..).  backward != 0: turned the other way, which
+ * takes the gradient of y to that of x.  y may be x (same strides); else they must not overlap.  dim: any from rot on. */
+int comet_rope(const comet_rope_plan *plan, comet_rows x, comet_rows y, uint32_t n_tokens, uint32_t heads, uint32_t dim, int dtype,
+               const int32_t *dev_positions, int backward, void *stream);
+
+/* Bytes of a cache, 0 if the shape is invalid. */
+uint64_t comet_cache_bytes(comet_cache_shape shape);
+
+/* Put the batch's keys and values into the cache: keys turned on the way (plan NULL: as they are) and rounded to dtype,
+ * complete blocks quantised.  dev_positions: int32[n_tokens], or NULL for the tokens' places in their sequences.  q, q_out, q_heads: the
+ * queries of the same tokens, turned in the same launch (q_heads 0: none; q_out may be q). */
+int comet_cache_append(void *dev_cache, comet_cache_shape shape, const comet_cache_batch *batch, uint32_t n_tokens, comet_rows k, comet_rows v,
+                       comet_rows q, comet_rows q_out, uint32_t q_heads, int dtype, const comet_rope_plan *plan,
+                       const int32_t *dev_positions, void *stream, int32_t *dev_status);
+
+/* Read the batch's tokens back as the cache holds them, in dtype. */
+int comet_cache_fetch(const void *dev_cache, comet_cache_shape shape, const comet_cache_batch *batch, uint32_t n_tokens, comet_rows k, comet_rows v,
+                      int dtype, void *stream, int32_t *dev_status);
+
+/* Attention of the batch's queries over the cache: out = softmax(scale * q k^T) v, query heads h * q_heads/heads .. sharing key/value head h.
+ * causal != 0: a query sees the tokens up to its own place (n queries are the last n of lens[b] tokens; those in front of
+ * the first see nothing); 0: all lens[b].  A row that sees nothing is 0 and its lse -Inf.  dev_lse: float32[n_tokens][q_heads],
+ * log of the sum of exp of the row's scores, or NULL.  scale: finite, >= 0.  dev_work: comet_cache_attend_work bytes, 16-byte aligned, whose contents
+ * need no initialisation; calls that can overlap in time need one each. */
+uint64_t comet_cache_attend_work(comet_cache_shape shape, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads);
+int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const comet_cache_batch *batch, uint32_t n_tokens, comet_rows q, uint32_t q_heads,
+                       int dtype, float scale, int causal, comet_rows out, float *dev_lse, void *dev_work, uint64_t work_bytes,
+                       void *stream, int32_t *dev_status);
+
 /* ---- stage-level entry points: each runs one step of the pipeline alone so
  * ---- that it can be compared with the reference implementation ------------ */
 

@@ -144,3 +144,25 @@ class saved_activations:
         decompress(packed.buf, packed.used, packed.shape, out, stream=torch.cuda.current_stream())
         self.unpacked += 1
         return out
+
+
+class _Rotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, rope, positions):
+        ctx.rope = rope
+        ctx.save_for_backward(positions)
+        return comet.comet_rope(x, rope, positions)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        if grad.stride(-1) != 1:
+            grad = grad.contiguous()
+        (positions,) = ctx.saved_tensors
+        return comet.comet_rope(grad, ctx.rope, positions, backward=True), None, None
+
+
+def rotate(x, rope: "comet.Rope", positions=None):
+    """x [tokens, heads, dim] turned by its tokens' positions (``comet.comet_rope``), differentiable.  The gradient is the rotation the other
+    way, so nothing but ``positions`` is kept for the backward pass."""
+    return _Rotate.apply(x, rope, positions)

@@ -21,6 +21,7 @@ EXPORTS = (
     "comet_create", "comet_destroy", "comet_set_chunk_syms", "comet_set_zero_chunks", "comet_compress_bound", "comet_compress", "comet_compress_with_codebook",
     "comet_decompress", "comet_decompress_static", "comet_compress_16", "comet_decompress_16", "comet_sync", "comet_peek", "comet_adapt_defaults", "comet_adapt_eb", "comet_abs_mean",
     "comet_controller_init", "comet_controller_tick", "comet_controller_update",
+    "comet_rope_steps", "comet_rope", "comet_cache_bytes", "comet_cache_append", "comet_cache_fetch", "comet_cache_attend_work", "comet_cache_attend",
     "comet_stage_quantize", "comet_stage_codebook", "comet_stage_encode", "comet_stage_decode",
     "comet_stage_reconstruct", "comet_profile_enable", "comet_profile_reset", "comet_profile_read", "comet_strerror",
 )
@@ -46,6 +47,28 @@ class LayerStats(C.Structure):
 
 class AdaptCfg(C.Structure):
     _fields_ = [("a", C.c_double), ("sigma_frac", C.c_double), ("eb_min", C.c_float), ("eb_max", C.c_float)]
+
+
+class CacheShape(C.Structure):
+    _fields_ = [("n_pages", C.c_uint32), ("page_tokens", C.c_uint32), ("n_slots", C.c_uint32), ("heads", C.c_uint32), ("dim", C.c_uint32)]
+
+
+class CacheBatch(C.Structure):
+    _fields_ = [("n_seqs", C.c_uint32), ("table_width", C.c_uint32), ("dev_starts", C.c_void_p), ("dev_lens", C.c_void_p),
+                ("dev_table", C.c_void_p), ("dev_slots", C.c_void_p)]
+
+
+class CacheRows(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class RopePlan(C.Structure):
+    _fields_ = [("rot", C.c_uint32), ("layout", C.c_uint32), ("amp", C.c_float), ("dev_steps", C.c_void_p)]
+
+
+class RopeCfg(C.Structure):
+    _fields_ = [("rot", C.c_uint32), ("scaling", C.c_uint32), ("base", C.c_double), ("factor", C.c_double), ("original_len", C.c_double),
+                ("beta_fast", C.c_double), ("beta_slow", C.c_double)]
 
 
 class CometError(RuntimeError):
@@ -87,6 +110,16 @@ def lib():
         L.comet_adapt_defaults.argtypes = [C.POINTER(AdaptCfg)]
         L.comet_adapt_defaults.restype = None
         L.comet_adapt_eb.argtypes = [C.POINTER(LayerStats), C.POINTER(AdaptCfg), C.POINTER(C.c_float)]
+        u32, i32 = C.c_uint32, C.c_int
+        batch, plan = C.POINTER(CacheBatch), C.POINTER(RopePlan)
+        L.comet_rope_steps.argtypes = [C.POINTER(RopeCfg), vp, C.POINTER(C.c_float)]
+        L.comet_rope.argtypes = [plan, CacheRows, CacheRows, u32, u32, u32, i32, vp, i32, vp]
+        L.comet_cache_bytes.argtypes = [CacheShape]
+        L.comet_cache_append.argtypes = [vp, CacheShape, batch, u32, CacheRows, CacheRows, CacheRows, CacheRows, u32, i32, plan, vp, vp, vp]
+        L.comet_cache_fetch.argtypes = [vp, CacheShape, batch, u32, CacheRows, CacheRows, i32, vp, vp]
+        L.comet_cache_attend_work.argtypes = [CacheShape, u32, u32, u32]
+        L.comet_cache_attend.argtypes = [vp, CacheShape, batch, u32, CacheRows, u32, i32, C.c_float, i32, CacheRows, vp, vp, u64, vp, vp]
+        L.comet_cache_bytes.restype = L.comet_cache_attend_work.restype = u64
         L.comet_stage_quantize.argtypes = [vp, vp, Shape, C.c_float, C.c_uint32, vp, vp, vp, vp, u64, vp]
         L.comet_stage_codebook.argtypes = [vp, vp, C.c_uint32, vp, vp, vp]
         L.comet_stage_encode.argtypes = [vp, vp, u64, C.c_uint32, C.c_uint32, vp, vp, vp, u64, vp]
@@ -98,7 +131,8 @@ def lib():
         L.comet_strerror.argtypes = [C.c_int]
         L.comet_strerror.restype = C.c_char_p
         for name in EXPORTS:
-            if name not in ("comet_destroy", "comet_compress_bound", "comet_adapt_defaults", "comet_strerror"):
+            if name not in ("comet_destroy", "comet_compress_bound", "comet_adapt_defaults", "comet_strerror", "comet_cache_bytes",
+                            "comet_cache_attend_work"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -321,3 +355,237 @@ class Context:
     def comet_stage_reconstruct(self, codes, records, n_records: int, shape, nbins: int, eb: float, out, stream=None) -> None:
         _chk(lib().comet_stage_reconstruct(self._h, _ptr(codes), _ptr(records), n_records, _shape(shape), nbins, C.c_float(eb),
                                            _stream(stream), _ptr(out)), "comet_stage_reconstruct")
+
+
+# ---- keys and values of attention layers ----------------------------------------------------------------------------
+F32 = 0
+CACHE_BLOCK = 32
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def _same_device(where: str, *tensors):
+    """The one device of the tensors (None among them is skipped)."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{where}: device tensors only")
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError(f"{where}: tensors on {device} and {t.device}")
+    return device
+
+
+class _On:
+    """Makes the tensors' device current for a call, and the call's stream where memory is allocated for its results (so that
+    the allocator knows which stream uses them); does nothing where both are so already."""
+    __slots__ = ("guards", "stream")
+
+    def __init__(self, device, stream):
+        import torch
+        self.guards = []
+        if device.index != torch.cuda.current_device():
+            self.guards.append(torch.cuda.device(device))
+        if stream is None:
+            self.stream = None
+        else:
+            if not hasattr(stream, "cuda_stream"):
+                stream = torch.cuda.ExternalStream(int(stream), device=device)
+            self.guards.append(torch.cuda.stream(stream))
+            self.stream = stream
+
+    def __enter__(self):
+        for g in self.guards:
+            g.__enter__()
+        import torch
+        return C.c_void_p((self.stream or torch.cuda.current_stream()).cuda_stream)
+
+    def __exit__(self, *exc):
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+
+
+def _int32(t, where: str, *shape):
+    if str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{where}: contiguous int32 tensor of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
+    return t
+
+
+def _rows3(t, where: str, heads=None, dim=None, tokens=None, dtype=None) -> CacheRows:
+    s = t.shape
+    if len(s) != 3 or (heads is not None and s[1] != heads) or (dim is not None and s[2] != dim) or (tokens is not None and s[0] != tokens):
+        raise ValueError(f"{where}: tensor of [tokens={tokens}, heads={heads}, dim={dim}] expected, got {tuple(s)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{where}: {dtype} expected, got {t.dtype}")
+    a, b, c = t.stride()
+    if c != 1 and s[2] > 1:
+        raise ValueError(f"{where}: the values of a head must be contiguous")
+    return CacheRows(t.data_ptr(), a, b)
+
+
+def _row_dtype(t) -> int:
+    return F32 if str(t.dtype) == "torch.float32" else _dtype16(t)
+
+
+def _status_ptr(status):
+    if status is None:
+        return None
+    if str(status.dtype) != "torch.int32" or status.numel() != 1:
+        raise ValueError("status: int32 tensor of one element expected")
+    return status.data_ptr()
+
+
+def comet_rope_steps(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_len: float = 4096,
+                     beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """(steps, amp) of a rotation: turns per position of every pair in units of 2^-64, the factor on the turned values."""
+    if scaling not in ROPE_SCALING:
+        raise ValueError(f"scaling: one of {sorted(ROPE_SCALING)} expected, got {scaling!r}")
+    cfg = RopeCfg(int(rot), ROPE_SCALING[scaling], base, factor, original_len, beta_fast, beta_slow)
+    steps, amp = (C.c_uint64 * max(1, int(rot) // 2))(), C.c_float()
+    _chk(lib().comet_rope_steps(C.byref(cfg), steps, C.byref(amp)), "comet_rope_steps")
+    return list(steps), amp.value
+
+
+class Rope:
+    """A rotation by positions, its steps in device memory: the first `rot` values of a head in pairs (i, i + rot/2), or (2i, 2i + 1)
+    if interleaved; scaling "none", "linear", "base" or "parts" for contexts `factor` times as long as original_len."""
+
+    def __init__(self, rot: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
+                 original_len: float = 4096, beta_fast: float = 32.0, beta_slow: float = 1.0, device=None):
+        import torch
+        steps, self.amp = comet_rope_steps(rot, base, scaling, factor, original_len, beta_fast, beta_slow)
+        self.rot, self.interleaved = int(rot), bool(interleaved)
+        self.steps = torch.tensor(steps, dtype=torch.int64).to(torch.device("cuda", torch.cuda.current_device()) if device is None else device)
+        self._plan = RopePlan(self.rot, 1 if interleaved else 0, self.amp, self.steps.data_ptr())
+
+
+def comet_rope(x, rope: Rope, positions=None, out=None, backward: bool = False, stream=None):
+    """x [tokens, heads, dim] (fp32, fp16 or bf16, any strides with contiguous heads) turned by its tokens' positions (int32, or None for
+    0, 1, ..); backward: the other way.  out: the result's tensor, x itself is fine."""
+    import torch
+    device = _same_device("comet_rope", x, positions, out, rope.steps)
+    rx = _rows3(x, "comet_rope: x")
+    tokens, heads, dim = x.shape
+    if positions is not None:
+        _int32(positions, "comet_rope: positions", tokens)
+    with _On(device, stream) as st:
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=device)
+        ry = _rows3(out, "comet_rope: out", heads, dim, tokens, x.dtype)
+        _chk(lib().comet_rope(C.byref(rope._plan), rx, ry, tokens, heads, dim, _row_dtype(x), None if positions is None else positions.data_ptr(),
+                              1 if backward else 0, st), "comet_rope")
+    return out
+
+
+class Batch:
+    """Which tokens of which sequences a call on a cache is about (int32 device tensors, read when the call runs): starts [n + 1], lens [n]
+    (tokens held once the batch's are in), table [n, pages], slots [n] or None."""
+
+    def __init__(self, starts, lens, table, slots=None):
+        self.device = _same_device("Batch", starts, lens, table, slots)
+        n = lens.shape[0]
+        self.tensors = (_int32(starts, "Batch: starts", n + 1), _int32(lens, "Batch: lens", n), _int32(table, "Batch: table", n, None),
+                        None if slots is None else _int32(slots, "Batch: slots", n))
+        self.n_seqs = n
+        self._c = CacheBatch(n, table.shape[1], starts.data_ptr(), lens.data_ptr(), table.data_ptr(), None if slots is None else slots.data_ptr())
+
+
+class Cache:
+    """Keys and values in blocks of 32 tokens, 8 bits a value; one device buffer."""
+
+    def __init__(self, n_pages: int, page_tokens: int, n_slots: int, heads: int, dim: int, buf=None, device=None):
+        import torch
+        self.shape = CacheShape(int(n_pages), int(page_tokens), int(n_slots), int(heads), int(dim))
+        self.heads, self.dim = int(heads), int(dim)
+        self.nbytes = comet_cache_bytes(n_pages, page_tokens, n_slots, heads, dim)
+        if not self.nbytes:
+            raise CometError(ERR_INVALID, "comet_cache_bytes")
+        if buf is None:
+            buf = torch.empty(self.nbytes, dtype=torch.uint8, device=torch.device("cuda", torch.cuda.current_device()) if device is None else device)
+        if str(buf.dtype) != "torch.uint8" or not buf.is_contiguous() or buf.numel() < self.nbytes:
+            raise ValueError(f"buf: contiguous uint8 tensor of {self.nbytes} bytes expected")
+        self.buf, self.device = buf, _same_device("Cache", buf)
+        self._p = C.c_void_p(buf.data_ptr())
+
+    def comet_cache_append(self, batch: Batch, k, v, rope: Rope | None = None, q=None, q_out=None, positions=None, status=None, stream=None):
+        """Put the batch's keys and values [tokens, heads, dim] (fp16 or bf16) into the cache, the keys turned by `rope` on the way.
+        q [tokens, query heads, dim]: turned as well, into q_out (a new tensor if None), which is returned."""
+        import torch
+        device = _same_device("comet_cache_append", self.buf, batch.tensors[0], k, v, q, q_out, positions, status, None if rope is None else rope.steps)
+        tokens, dt = k.shape[0], k.dtype
+        rk = _rows3(k, "comet_cache_append: k", self.heads, self.dim)
+        rv = _rows3(v, "comet_cache_append: v", self.heads, self.dim, tokens, dt)
+        if positions is not None:
+            _int32(positions, "comet_cache_append: positions", tokens)
+        if q is None and q_out is not None:
+            raise ValueError("comet_cache_append: q_out without q")
+        with _On(device, stream) as st:
+            q_heads, rq, ro = 0, CacheRows(), CacheRows()
+            if q is not None:
+                rq = _rows3(q, "comet_cache_append: q", None, self.dim, tokens, dt)
+                q_heads = q.shape[1]
+                if q_out is None:
+                    q_out = torch.empty(q.shape, dtype=dt, device=device)
+                ro = _rows3(q_out, "comet_cache_append: q_out", q_heads, self.dim, tokens, dt)
+            _chk(lib().comet_cache_append(self._p, self.shape, C.byref(batch._c), tokens, rk, rv, rq, ro, q_heads, _dtype16(k),
+                                          None if rope is None else C.byref(rope._plan), None if positions is None else positions.data_ptr(), st,
+                                          _status_ptr(status)), "comet_cache_append")
+        return q_out
+
+    def comet_cache_fetch(self, batch: Batch, k=None, v=None, dtype=None, tokens: int | None = None, status=None, stream=None):
+        """The batch's keys and values as the cache holds them, (k, v): into the tensors given, or new ones of `dtype` with `tokens` rows (those
+        that belong to no sequence stay as the allocator left them)."""
+        import torch
+        device = _same_device("comet_cache_fetch", self.buf, batch.tensors[0], k, v, status)
+        with _On(device, stream) as st:
+            if k is None or v is None:
+                if tokens is None:
+                    tokens = (v if k is None else k).shape[0]
+                if dtype is None:
+                    dtype = (v if k is None else k).dtype
+                k = torch.empty((tokens, self.heads, self.dim), dtype=dtype, device=device) if k is None else k
+                v = torch.empty((tokens, self.heads, self.dim), dtype=dtype, device=device) if v is None else v
+            rk = _rows3(k, "comet_cache_fetch: k", self.heads, self.dim, tokens, dtype)
+            rv = _rows3(v, "comet_cache_fetch: v", self.heads, self.dim, k.shape[0], k.dtype)
+            _chk(lib().comet_cache_fetch(self._p, self.shape, C.byref(batch._c), k.shape[0], rk, rv, _dtype16(k), st, _status_ptr(status)),
+                 "comet_cache_fetch")
+        return k, v
+
+    def comet_cache_attend(self, batch: Batch, q, out=None, lse=None, scale: float | None = None, causal: bool = True, work=None, status=None,
+                           stream=None):
+        """Attention of the batch's queries [tokens, query heads, dim] over the cache; scale: 1 / sqrt(dim) if None.  lse: a float32 tensor
+        [tokens, query heads] for the log-sum-exp of every row, or True for a new one; then (out, lse) is returned, else out.  work: uint8 tensor
+        of comet_cache_attend_work bytes, allocated if None."""
+        import torch
+        device = _same_device("comet_cache_attend", self.buf, batch.tensors[0], q, out, None if lse is True else lse, work, status)
+        rq = _rows3(q, "comet_cache_attend: q", None, self.dim)
+        tokens, q_heads = q.shape[0], q.shape[1]
+        need = int(lib().comet_cache_attend_work(self.shape, batch.n_seqs, tokens, q_heads))
+        if not need:
+            raise CometError(ERR_INVALID, "comet_cache_attend_work")
+        with _On(device, stream) as st:
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=device)
+            ro = _rows3(out, "comet_cache_attend: out", q_heads, self.dim, tokens, q.dtype)
+            if lse is True:
+                lse = torch.empty((tokens, q_heads), dtype=torch.float32, device=device)
+            elif lse is not None and (str(lse.dtype) != "torch.float32" or not lse.is_contiguous() or tuple(lse.shape) != (tokens, q_heads)):
+                raise ValueError("comet_cache_attend: lse: contiguous float32 tensor [tokens, query heads] expected")
+            if work is None:
+                work = torch.empty(need, dtype=torch.uint8, device=device)
+            elif not work.is_contiguous():
+                raise ValueError("comet_cache_attend: work: contiguous tensor expected")
+            _chk(lib().comet_cache_attend(self._p, self.shape, C.byref(batch._c), tokens, rq, q_heads, _dtype16(q),
+                                          self.dim ** -0.5 if scale is None else scale, 1 if causal else 0, ro, None if lse is None else lse.data_ptr(),
+                                          work.data_ptr(), work.numel() * work.element_size(), st, _status_ptr(status)), "comet_cache_attend")
+        return out if lse is None else (out, lse)
+
+
+def comet_cache_bytes(n_pages: int, page_tokens: int, n_slots: int, heads: int, dim: int) -> int:
+    return int(lib().comet_cache_bytes(CacheShape(int(n_pages), int(page_tokens), int(n_slots), int(heads), int(dim))))
+
+
+def comet_cache_attend_work(cache: Cache, n_seqs: int, n_tokens: int, q_heads: int) -> int:
+    return int(lib().comet_cache_attend_work(cache.shape, int(n_seqs), int(n_tokens), int(q_heads)))

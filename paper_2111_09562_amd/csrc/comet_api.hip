@@ -16,14 +16,15 @@
 
 using namespace comet;
 
-namespace {
+static thread_local char g_hip_msg[256] = "no HIP error recorded";
 
-thread_local char g_hip_msg[256] = "no HIP error recorded";
-
-int hip_fail(hipError_t e, const char *what) {
+int comet::hip_fail(hipError_t e, const char *what) {
     snprintf(g_hip_msg, sizeof(g_hip_msg), "%s: %s", what, hipGetErrorString(e));
     return COMET_ERR_HIP;
 }
+
+namespace {
+
 #define HIP_TRY(expr)                                                   \
     do {                                                                \
         hipError_t e_ = (expr);                                         \

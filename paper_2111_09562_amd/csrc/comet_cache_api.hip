@@ -1,0 +1,257 @@
+// Host side of the compressed key/value cache: argument checks, launch geometry and the entry points of include/comet.h.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "comet_cache.h"
+
+using namespace comet;
+
+namespace {
+
+#define HIP_TRY(expr)                                                   \
+    do {                                                                \
+        hipError_t e_ = (expr);                                         \
+        if (e_ != hipSuccess) return hip_fail(e_, #expr);               \
+    } while (0)
+
+constexpr uint32_t kMaxHeads = 4096, kMaxQueryHeads = 16384, kMaxSeqs = 1u << 24, kMaxRopeDim = 4096;
+constexpr uint64_t kMaxRows = 0x7fffffffull;
+
+bool valid_shape(comet_cache_shape s) {
+    return s.n_pages && s.n_pages <= 0x7fffffffu && s.page_tokens && s.page_tokens % kBlk == 0u && s.page_tokens <= (1u << 20) && s.n_slots &&
+           s.n_slots <= 0x7fffffffu && s.heads && s.heads <= kMaxHeads && s.dim && s.dim % 32u == 0u && s.dim <= kCacheMaxDim;
+}
+// Blocks of all pages and heads; false beyond 2^40 (or of the open blocks), far behind any memory.
+bool count_blocks(comet_cache_shape s, uint64_t *n) {
+    const uint64_t a = (uint64_t)s.n_pages * s.heads;                           // < 2^43
+    if (a > (1ull << 40) || (uint64_t)s.n_slots * s.heads > (1ull << 40)) return false;
+    *n = a * (s.page_tokens / kBlk);                                            // < 2^55
+    return *n <= (1ull << 40);
+}
+inline uint64_t pad256(uint64_t v) { return (v + 255ull) / 256ull * 256ull; }
+
+bool cache_args(const void *dev, comet_cache_shape s, CacheArgs *c) {
+    uint64_t n;
+    if (!dev || (uintptr_t)dev % 16u || !valid_shape(s) || !count_blocks(s, &n)) return false;
+    uint8_t *p = const_cast<uint8_t *>(static_cast<const uint8_t *>(dev));
+    c->blocks = p;
+    c->scales = reinterpret_cast<float *>(p + n * 64u * s.dim);
+    c->ring = p + n * 64u * s.dim + pad256(n * 8u);
+    c->n_pages = s.n_pages; c->per = s.page_tokens / kBlk; c->n_slots = s.n_slots; c->heads = s.heads; c->dim = s.dim;
+    return true;
+}
+bool batch_args(const comet_cache_batch *b, uint32_t n_tokens, int32_t *status, BatchArgs *a) {
+    if (!b || b->n_seqs > kMaxSeqs || n_tokens > kMaxRows) return false;
+    if (n_tokens && (!b->n_seqs || !b->table_width || !b->dev_starts || !b->dev_lens || !b->dev_table)) return false;
+    for (const void *p : {(const void *)b->dev_starts, (const void *)b->dev_lens, (const void *)b->dev_table, (const void *)b->dev_slots, (const void *)status})
+        if ((uintptr_t)p % 4u) return false;
+    a->starts = b->dev_starts; a->lens = b->dev_lens; a->table = b->dev_table; a->slots = b->dev_slots;
+    a->width = b->table_width; a->n_seqs = b->n_seqs; a->n_tokens = n_tokens; a->status = status;
+    return true;
+}
+inline uint32_t elem_size(int dtype) { return dtype == COMET_F32 ? 4u : 2u; }
+bool rows_args(comet_rows r, int dtype, Rows *to) {
+    if (!r.dev || (uintptr_t)r.dev % elem_size(dtype)) return false;
+    to->p = static_cast<uint8_t *>(r.dev); to->token = r.token_stride; to->head = r.head_stride;
+    return true;
+}
+bool rows_aligned(const Rows &r, int dtype) {                                   // every row begins at a multiple of 16 bytes
+    const int64_t v = 16 / elem_size(dtype);
+    return (uintptr_t)r.p % 16u == 0u && r.token % v == 0 && r.head % v == 0;
+}
+bool rope_args(const comet_rope_plan *p, uint32_t dim, const int32_t *positions, RopeArgs *r) {
+    *r = RopeArgs{};
+    if (!p) return true;
+    if (!p->dev_steps || (uintptr_t)p->dev_steps % 8u || p->rot < 2u || p->rot % 2u || p->rot > dim || p->layout > COMET_ROPE_PAIRS ||
+        !std::isfinite(p->amp) || (uintptr_t)positions % 4u) return false;
+    r->steps = p->dev_steps; r->positions = positions; r->rot = p->rot; r->interleaved = p->layout == COMET_ROPE_PAIRS; r->amp = p->amp;
+    return true;
+}
+inline uint32_t block_units(const BatchArgs &b) { return b.n_tokens / kBlk + 2u * b.n_seqs; }      // < 2^26 + 2^25 (first_unit)
+
+template <typename T, int V>
+void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tokens, uint32_t heads, uint32_t dim, bool in_place, uint32_t sign, hipStream_t st) {
+    RopeGrid g;
+    g.rot_chunks = r.rot / (2u * V);
+    g.chunks = g.rot_chunks + (in_place ? 0u : (dim - r.rot) / V);
+    // up to eight heads share a chunk's sines, while that leaves a thousand workgroups
+    const uint64_t threads = (uint64_t)n_tokens * heads * g.chunks;
+    uint64_t per = threads / (1024u * kRopeBlock);
+    per = per < 1u ? 1u : (per > 8u ? 8u : per);
+    g.groups = (uint32_t)((heads + per - 1u) / per);
+    g.per_token = g.groups * g.chunks;
+    g.tokens_wg = g.per_token <= (uint32_t)kRopeBlock ? kRopeBlock / g.per_token : 0u;
+    const uint32_t wg = g.tokens_wg ? (n_tokens - 1u) / g.tokens_wg + 1u : n_tokens;
+    k_rope<T, V><<<wg, kRopeBlock, 0, st>>>(r, g, x, y, n_tokens, heads, dim, sign);
+}
+
+constexpr uint32_t kAttendPieces = 1024;                 // workgroups an attention call is cut into, about
+struct AttendPlan {
+    uint32_t pieces, slots, tiles;
+    uint64_t off_s, off_dir, bytes;
+};
+bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads, AttendPlan *p) {
+    if (!valid_shape(s) || !q_heads || q_heads > kMaxQueryHeads || q_heads % s.heads || n_seqs > kMaxSeqs) return false;
+    const uint64_t rows = (uint64_t)n_tokens * (q_heads / s.heads);
+    if (rows > kMaxRows) return false;
+    p->tiles = (uint32_t)(rows / 32u) + n_seqs;
+    p->pieces = (kAttendPieces + s.heads - 1u) / s.heads;
+    p->slots = p->pieces + p->tiles;
+    const uint64_t n = (uint64_t)p->slots * s.heads;
+    if (n > kMaxRows) return false;
+    p->off_s = n * 32u * s.dim * 4u;
+    p->off_dir = p->off_s + n * 32u * 3u * 4u;
+    p->bytes = p->off_dir + 8ull * (p->tiles + 1ull);
+    return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+int comet_rope_steps(const comet_rope_cfg *cfg, uint64_t *host_steps, float *amp) {
+    if (!cfg || !host_steps || !amp) return COMET_ERR_INVALID;
+    const comet_rope_cfg c = *cfg;
+    if (c.rot < 2u || c.rot % 2u || c.rot > kMaxRopeDim || c.scaling > COMET_ROPE_PARTS || !std::isfinite(c.base) || !(c.base > 1.0) ||
+        !std::isfinite(c.factor) || !(c.factor >= 1.0)) return COMET_ERR_INVALID;
+    if (c.scaling == COMET_ROPE_PARTS && (!std::isfinite(c.original_len) || !(c.original_len > 0.0) || !std::isfinite(c.beta_fast) ||
+        !(c.beta_slow >= 0.0) || !(c.beta_fast > c.beta_slow))) return COMET_ERR_INVALID;
+    const long double two_pi = 6.283185307179586476925286766559005768L;
+    long double base = c.base;
+    const long double factor = c.factor;
+    if (c.scaling == COMET_ROPE_BASE) base *= c.rot > 2u ? powl(factor, (long double)c.rot / (c.rot - 2u)) : factor;
+    for (uint32_t i = 0; i < c.rot / 2u; ++i) {
+        long double f = powl(base, -2.0L * i / c.rot);
+        if (c.scaling == COMET_ROPE_LINEAR) f /= factor;
+        if (c.scaling == COMET_ROPE_PARTS) {
+            const long double turns = c.original_len * f / two_pi;
+            long double keep = (turns - c.beta_slow) / ((long double)c.beta_fast - c.beta_slow);
+            keep = keep < 0.0L ? 0.0L : (keep > 1.0L ? 1.0L : keep);
+            f *= keep + (1.0L - keep) / factor;
+        }
+        host_steps[i] = (uint64_t)roundl(f / two_pi * 0x1p64L);                  // f <= 1 radian: less than a sixth of a turn
+    }
+    *amp = c.scaling == COMET_ROPE_PARTS ? (float)(0.1 * std::log(c.factor) + 1.0) : 1.0f;
+    return COMET_OK;
+}
+
+int comet_rope(const comet_rope_plan *plan, comet_rows x, comet_rows y, uint32_t n_tokens, uint32_t heads, uint32_t dim, int dtype,
+               const int32_t *dev_positions, int backward, void *stream) {
+    RopeArgs r;
+    Rows rx, ry;
+    if (!plan || dtype < COMET_F32 || dtype > COMET_BF16 || !heads || heads > kMaxQueryHeads || dim > kMaxRopeDim || n_tokens > kMaxRows ||
+        !rope_args(plan, dim, dev_positions, &r)) return COMET_ERR_INVALID;
+    if (!n_tokens) return COMET_OK;
+    if (!rows_args(x, dtype, &rx) || !rows_args(y, dtype, &ry)) return COMET_ERR_INVALID;
+    const bool in_place = x.dev == y.dev;
+    if (in_place && (x.token_stride != y.token_stride || x.head_stride != y.head_stride)) return COMET_ERR_INVALID;
+    const uint32_t v = 16u / elem_size(dtype);
+    const bool vec = r.rot % (2u * v) == 0u && (dim - r.rot) % v == 0u && rows_aligned(rx, dtype) && rows_aligned(ry, dtype);
+    const uint32_t sign = backward ? 0x80000000u : 0u;
+    hipStream_t st = (hipStream_t)stream;
+    if (dtype == COMET_F32) {
+        if (vec) launch_rope<float, 4>(r, rx, ry, n_tokens, heads, dim, in_place, sign, st);
+        else launch_rope<float, 1>(r, rx, ry, n_tokens, heads, dim, in_place, sign, st);
+    } else if (dtype == COMET_F16) {
+        if (vec) launch_rope<_Float16, 8>(r, rx, ry, n_tokens, heads, dim, in_place, sign, st);
+        else launch_rope<_Float16, 1>(r, rx, ry, n_tokens, heads, dim, in_place, sign, st);
+    } else {
+        if (vec) launch_rope<__bf16, 8>(r, rx, ry, n_tokens, heads, dim, in_place, sign, st);
+        else launch_rope<__bf16, 1>(r, rx, ry, n_tokens, heads, dim, in_place, sign, st);
+    }
+    HIP_TRY(hipGetLastError());
+    return COMET_OK;
+}
+
+uint64_t comet_cache_bytes(comet_cache_shape s) {
+    uint64_t n;
+    if (!valid_shape(s) || !count_blocks(s, &n)) return 0;
+    return n * 64u * s.dim + pad256(n * 8u) + (uint64_t)s.n_slots * s.heads * 2u * ring_half_bytes(s.dim);
+}
+
+int comet_cache_append(void *dev_cache, comet_cache_shape shape, const comet_cache_batch *batch, uint32_t n_tokens, comet_rows k, comet_rows v,
+                       comet_rows q, comet_rows q_out, uint32_t q_heads, int dtype, const comet_rope_plan *plan,
+                       const int32_t *dev_positions, void *stream, int32_t *dev_status) {
+    AppendArgs a{};
+    if ((dtype != COMET_F16 && dtype != COMET_BF16) || q_heads > kMaxQueryHeads || !cache_args(dev_cache, shape, &a.c) ||
+        !batch_args(batch, n_tokens, dev_status, &a.b) || !rope_args(plan, shape.dim, dev_positions, &a.rope)) return COMET_ERR_INVALID;
+    if (!n_tokens) return COMET_OK;
+    if (!rows_args(k, dtype, &a.k) || !rows_args(v, dtype, &a.v)) return COMET_ERR_INVALID;
+    a.vec = rows_aligned(a.k, dtype) && rows_aligned(a.v, dtype) && a.rope.rot % 16u == 0u;
+    a.q_heads = q_heads;
+    uint32_t q_wg = 0;
+    if (q_heads) {
+        if (!rows_args(q, dtype, &a.q) || !rows_args(q_out, dtype, &a.q_out)) return COMET_ERR_INVALID;
+        if (q.dev == q_out.dev && (q.token_stride != q_out.token_stride || q.head_stride != q_out.head_stride)) return COMET_ERR_INVALID;
+        a.vec = a.vec && rows_aligned(a.q, dtype) && rows_aligned(a.q_out, dtype);
+        a.q_heads_wg = 8u;
+        q_wg = (q_heads + a.q_heads_wg - 1u) / a.q_heads_wg;
+    }
+    const dim3 grid(block_units(a.b), shape.heads + q_wg);
+    hipStream_t st = (hipStream_t)stream;
+    if (dtype == COMET_F16) k_cache_append<_Float16><<<grid, kCacheBlock, cache_lds(shape.dim), st>>>(a);
+    else k_cache_append<__bf16><<<grid, kCacheBlock, cache_lds(shape.dim), st>>>(a);
+    HIP_TRY(hipGetLastError());
+    return COMET_OK;
+}
+
+int comet_cache_fetch(const void *dev_cache, comet_cache_shape shape, const comet_cache_batch *batch, uint32_t n_tokens, comet_rows k, comet_rows v,
+                      int dtype, void *stream, int32_t *dev_status) {
+    FetchArgs a{};
+    if ((dtype != COMET_F16 && dtype != COMET_BF16) || !cache_args(dev_cache, shape, &a.c) || !batch_args(batch, n_tokens, dev_status, &a.b))
+        return COMET_ERR_INVALID;
+    if (!n_tokens) return COMET_OK;
+    if (!rows_args(k, dtype, &a.k) || !rows_args(v, dtype, &a.v)) return COMET_ERR_INVALID;
+    a.vec = rows_aligned(a.k, dtype) && rows_aligned(a.v, dtype);
+    const dim3 grid(block_units(a.b), shape.heads);
+    hipStream_t st = (hipStream_t)stream;
+    if (dtype == COMET_F16) k_cache_fetch<_Float16><<<grid, kCacheBlock, cache_lds(shape.dim), st>>>(a);
+    else k_cache_fetch<__bf16><<<grid, kCacheBlock, cache_lds(shape.dim), st>>>(a);
+    HIP_TRY(hipGetLastError());
+    return COMET_OK;
+}
+
+uint64_t comet_cache_attend_work(comet_cache_shape shape, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads) {
+    AttendPlan p;
+    return plan_attend(shape, n_seqs, n_tokens, q_heads, &p) ? p.bytes : 0;
+}
+
+int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const comet_cache_batch *batch, uint32_t n_tokens, comet_rows q, uint32_t q_heads,
+                       int dtype, float scale, int causal, comet_rows out, float *dev_lse, void *dev_work, uint64_t work_bytes,
+                       void *stream, int32_t *dev_status) {
+    AttendArgs a{};
+    AttendPlan p;
+    if ((dtype != COMET_F16 && dtype != COMET_BF16) || !cache_args(dev_cache, shape, &a.c) || !batch_args(batch, n_tokens, dev_status, &a.b) ||
+        !std::isfinite(scale * 1.4426950408889634f) || scale < 0.0f || (uintptr_t)dev_lse % 4u || !plan_attend(shape, batch->n_seqs, n_tokens, q_heads, &p))
+        return COMET_ERR_INVALID;
+    if (!n_tokens) return COMET_OK;
+    if (!rows_args(q, dtype, &a.q) || !rows_args(out, dtype, &a.out) || !dev_work || (uintptr_t)dev_work % 16u) return COMET_ERR_INVALID;
+    if (work_bytes < p.bytes) return COMET_ERR_NOMEM;
+    a.lse = dev_lse; a.q_heads = q_heads; a.group = q_heads / shape.heads;
+    a.bf16 = dtype == COMET_BF16; a.causal = causal != 0; a.vec = rows_aligned(a.q, dtype) && rows_aligned(a.out, dtype);
+    a.pieces = p.pieces; a.slots = p.slots; a.scale = scale * 1.4426950408889634f;
+    uint8_t *w = static_cast<uint8_t *>(dev_work);
+    a.part_o = reinterpret_cast<float *>(w);
+    a.part_s = reinterpret_cast<float *>(w + p.off_s);
+    a.directory = reinterpret_cast<int32_t *>(w + p.off_dir);
+    hipStream_t st = (hipStream_t)stream;
+    const uint32_t wg = p.slots * shape.heads;
+    switch (shape.dim / 32u) {
+        case 1: k_attend<1><<<wg, kAttendBlock, 0, st>>>(a); break;
+        case 2: k_attend<2><<<wg, kAttendBlock, 0, st>>>(a); break;
+        case 3: k_attend<3><<<wg, kAttendBlock, 0, st>>>(a); break;
+        case 4: k_attend<4><<<wg, kAttendBlock, 0, st>>>(a); break;
+        case 5: k_attend<5><<<wg, kAttendBlock, 0, st>>>(a); break;
+        case 6: k_attend<6><<<wg, kAttendBlock, 0, st>>>(a); break;
+        case 7: k_attend<7><<<wg, kAttendBlock, 0, st>>>(a); break;
+        default: k_attend<8><<<wg, kAttendBlock, 0, st>>>(a); break;
+    }
+    HIP_TRY(hipGetLastError());
+    k_attend_join<<<p.tiles * shape.heads, kAttendBlock, 0, st>>>(a);
+    HIP_TRY(hipGetLastError());
+    return COMET_OK;
+}
+
+}  // extern "C"

@@ -13,6 +13,9 @@ constexpr int kWave = 64;                   // CDNA wavefront width
 // device-side status bits, latched in Control::status
 enum : uint32_t { ST_CAPACITY = 1u, ST_FORMAT = 2u, ST_INTERNAL = 4u, ST_CODEBOOK = 8u };
 
+// A failed HIP call: its error code, and its text for comet_strerror.
+int hip_fail(hipError_t e, const char *what);
+
 // Container header.  Field order is the on-disk order (little-endian).
 struct Header {
     uint32_t magic, version, status, N, C, H, W, nbins;

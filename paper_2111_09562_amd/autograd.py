@@ -148,21 +148,25 @@ class saved_activations:
 
 class _Rotate(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, rope, positions):
-        ctx.rope = rope
+    def forward(ctx, x, rope, positions, backward):
+        ctx.rope, ctx.turned_back = rope, backward
         ctx.save_for_backward(positions)
-        return comet.comet_rope(x, rope, positions)
+        return comet.comet_rope(x, rope, positions, backward=backward)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
+        (positions,) = ctx.saved_tensors
         if grad.stride(-1) != 1:
             grad = grad.contiguous()
-        (positions,) = ctx.saved_tensors
-        return comet.comet_rope(grad, ctx.rope, positions, backward=True), None, None
+        turn = _Rotate.apply if torch.is_grad_enabled() else _turn            # (a gradient of the gradient is asked for)
+        return turn(grad, ctx.rope, positions, not ctx.turned_back), None, None, None
+
+
+def _turn(x, rope, positions, backward):
+    return comet.comet_rope(x, rope, positions, backward=backward)
 
 
 def rotate(x, rope: "comet.Rope", positions=None):
     """x [tokens, heads, dim] turned by its tokens' positions (``comet.comet_rope``), differentiable.  The gradient is the rotation the other
     way, so nothing but ``positions`` is kept for the backward pass."""
-    return _Rotate.apply(x, rope, positions)
+    return _Rotate.apply(x, rope, positions, False)

@@ -363,64 +363,48 @@ CACHE_BLOCK = 32
 ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 
 
-def _same_device(where: str, *tensors):
-    """The one device of the tensors (None among them is skipped)."""
-    device = None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError(f"{where}: device tensors only")
-        if device is None:
-            device = t.device
-        elif t.device != device:
-            raise ValueError(f"{where}: tensors on {device} and {t.device}")
-    return device
+def _elsewhere(dev: int, stream):
+    """Contexts that make the tensors' device current and, where a stream is given, that stream: memory for results then comes from the
+    allocator's pool of the stream that uses it.  None where the call can go ahead as it is."""
+    import torch
+    if dev < 0:
+        raise ValueError("device tensors only")
+    if stream is None:
+        return None if torch._C._cuda_getDevice() == dev else torch.cuda.device(dev)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=torch.device("cuda", dev)) if int(stream) else torch.cuda.default_stream(dev)
+    if stream.device.index != dev:
+        raise ValueError(f"a stream of device {stream.device.index} for tensors on device {dev}")
+    return torch.cuda.stream(stream)                 # (makes the stream's device current, too)
 
 
-class _On:
-    """Makes the tensors' device current for a call, and the call's stream where memory is allocated for its results (so that
-    the allocator knows which stream uses them); does nothing where both are so already."""
-    __slots__ = ("guards", "stream")
-
-    def __init__(self, device, stream):
-        import torch
-        self.guards = []
-        if device.index != torch.cuda.current_device():
-            self.guards.append(torch.cuda.device(device))
-        if stream is None:
-            self.stream = None
-        else:
-            if not hasattr(stream, "cuda_stream"):
-                stream = torch.cuda.ExternalStream(int(stream), device=device)
-            self.guards.append(torch.cuda.stream(stream))
-            self.stream = stream
-
-    def __enter__(self):
-        for g in self.guards:
-            g.__enter__()
-        import torch
-        return C.c_void_p((self.stream or torch.cuda.current_stream()).cuda_stream)
-
-    def __exit__(self, *exc):
-        for g in reversed(self.guards):
-            g.__exit__(*exc)
+def _raw_stream(dev: int) -> int:
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _int32(t, where: str, *shape):
+def _int32(t, where: str, dev: int, *shape):
+    """Device pointer of a contiguous int32 tensor of that shape (None: any) on that device."""
     if str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
         raise ValueError(f"{where}: contiguous int32 tensor of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
-    return t
+    if t.get_device() != dev:
+        raise ValueError(f"{where}: on another device than the other tensors")
+    return t.data_ptr()
 
 
-def _rows3(t, where: str, heads=None, dim=None, tokens=None, dtype=None) -> CacheRows:
+def _rows3(t, where: str, dev: int, tokens, heads, dim, dtype) -> CacheRows:
+    """A [tokens, heads, dim] tensor (None: any) of a type on a device, its heads' values contiguous."""
+    if t.dim() != 3:
+        raise ValueError(f"{where}: tensor of three dimensions expected, got {tuple(t.shape)}")
     s = t.shape
-    if len(s) != 3 or (heads is not None and s[1] != heads) or (dim is not None and s[2] != dim) or (tokens is not None and s[0] != tokens):
+    if s[0] != tokens or (heads is not None and s[1] != heads) or s[2] != dim:
         raise ValueError(f"{where}: tensor of [tokens={tokens}, heads={heads}, dim={dim}] expected, got {tuple(s)}")
-    if dtype is not None and t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{where}: {dtype} expected, got {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{where}: on another device than the other tensors")
     a, b, c = t.stride()
-    if c != 1 and s[2] > 1:
+    if c != 1 and dim > 1:
         raise ValueError(f"{where}: the values of a head must be contiguous")
     return CacheRows(t.data_ptr(), a, b)
 
@@ -429,11 +413,11 @@ def _row_dtype(t) -> int:
     return F32 if str(t.dtype) == "torch.float32" else _dtype16(t)
 
 
-def _status_ptr(status):
+def _status_ptr(status, dev: int):
     if status is None:
         return None
-    if str(status.dtype) != "torch.int32" or status.numel() != 1:
-        raise ValueError("status: int32 tensor of one element expected")
+    if str(status.dtype) != "torch.int32" or status.numel() != 1 or status.get_device() != dev:
+        raise ValueError("status: int32 tensor of one element on the device of the others expected")
     return status.data_ptr()
 
 
@@ -458,24 +442,29 @@ class Rope:
         steps, self.amp = comet_rope_steps(rot, base, scaling, factor, original_len, beta_fast, beta_slow)
         self.rot, self.interleaved = int(rot), bool(interleaved)
         self.steps = torch.tensor(steps, dtype=torch.int64).to(torch.device("cuda", torch.cuda.current_device()) if device is None else device)
+        self.device_index = self.steps.get_device()
         self._plan = RopePlan(self.rot, 1 if interleaved else 0, self.amp, self.steps.data_ptr())
 
 
 def comet_rope(x, rope: Rope, positions=None, out=None, backward: bool = False, stream=None):
     """x [tokens, heads, dim] (fp32, fp16 or bf16, any strides with contiguous heads) turned by its tokens' positions (int32, or None for
     0, 1, ..); backward: the other way.  out: the result's tensor, x itself is fine."""
-    import torch
-    device = _same_device("comet_rope", x, positions, out, rope.steps)
-    rx = _rows3(x, "comet_rope: x")
+    dev = x.get_device()
+    on = _elsewhere(dev, stream)
+    if on is not None:
+        with on:
+            return comet_rope(x, rope, positions, out, backward)
+    if x.dim() != 3:
+        raise ValueError(f"comet_rope: x [tokens, heads, dim] expected, got {tuple(x.shape)}")
     tokens, heads, dim = x.shape
-    if positions is not None:
-        _int32(positions, "comet_rope: positions", tokens)
-    with _On(device, stream) as st:
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=device)
-        ry = _rows3(out, "comet_rope: out", heads, dim, tokens, x.dtype)
-        _chk(lib().comet_rope(C.byref(rope._plan), rx, ry, tokens, heads, dim, _row_dtype(x), None if positions is None else positions.data_ptr(),
-                              1 if backward else 0, st), "comet_rope")
+    rx = _rows3(x, "comet_rope: x", dev, tokens, heads, dim, x.dtype)
+    if out is None:
+        out = x.new_empty((tokens, heads, dim))
+    ry = _rows3(out, "comet_rope: out", dev, tokens, heads, dim, x.dtype)
+    if rope.device_index != dev:
+        raise ValueError("comet_rope: the rotation's steps are on another device")
+    pos = None if positions is None else _int32(positions, "comet_rope: positions", dev, tokens)
+    _chk(lib().comet_rope(rope._plan, rx, ry, tokens, heads, dim, _row_dtype(x), pos, 1 if backward else 0, _raw_stream(dev)), "comet_rope")
     return out
 
 
@@ -484,16 +473,17 @@ class Batch:
     (tokens held once the batch's are in), table [n, pages], slots [n] or None."""
 
     def __init__(self, starts, lens, table, slots=None):
-        self.device = _same_device("Batch", starts, lens, table, slots)
-        n = lens.shape[0]
-        self.tensors = (_int32(starts, "Batch: starts", n + 1), _int32(lens, "Batch: lens", n), _int32(table, "Batch: table", n, None),
-                        None if slots is None else _int32(slots, "Batch: slots", n))
-        self.n_seqs = n
-        self._c = CacheBatch(n, table.shape[1], starts.data_ptr(), lens.data_ptr(), table.data_ptr(), None if slots is None else slots.data_ptr())
+        dev = self.device_index = lens.get_device()
+        if dev < 0:
+            raise ValueError("Batch: device tensors only")
+        n = self.n_seqs = lens.shape[0]
+        self.tensors = (starts, lens, table, slots)
+        self._c = CacheBatch(n, table.shape[1], _int32(starts, "Batch: starts", dev, n + 1), _int32(lens, "Batch: lens", dev, n),
+                             _int32(table, "Batch: table", dev, n, None), None if slots is None else _int32(slots, "Batch: slots", dev, n))
 
 
 class Cache:
-    """Keys and values in blocks of 32 tokens, 8 bits a value; one device buffer."""
+    """Keys and values in blocks of 32 tokens, 8 bits a value; one device buffer (`buf`: uint8, allocated if None)."""
 
     def __init__(self, n_pages: int, page_tokens: int, n_slots: int, heads: int, dim: int, buf=None, device=None):
         import torch
@@ -504,53 +494,67 @@ class Cache:
             raise CometError(ERR_INVALID, "comet_cache_bytes")
         if buf is None:
             buf = torch.empty(self.nbytes, dtype=torch.uint8, device=torch.device("cuda", torch.cuda.current_device()) if device is None else device)
-        if str(buf.dtype) != "torch.uint8" or not buf.is_contiguous() or buf.numel() < self.nbytes:
-            raise ValueError(f"buf: contiguous uint8 tensor of {self.nbytes} bytes expected")
-        self.buf, self.device = buf, _same_device("Cache", buf)
-        self._p = C.c_void_p(buf.data_ptr())
+        if str(buf.dtype) != "torch.uint8" or not buf.is_contiguous() or buf.numel() < self.nbytes or not buf.is_cuda:
+            raise ValueError(f"buf: contiguous uint8 device tensor of {self.nbytes} bytes expected")
+        self.buf, self.device_index = buf, buf.get_device()
+        self._p = buf.data_ptr()
+
+    def _same(self, where: str, batch: Batch, rope=None) -> int:
+        dev = self.device_index
+        if batch.device_index != dev or (rope is not None and rope.device_index != dev):
+            raise ValueError(f"{where}: cache, batch and rotation on different devices")
+        return dev
 
     def comet_cache_append(self, batch: Batch, k, v, rope: Rope | None = None, q=None, q_out=None, positions=None, status=None, stream=None):
         """Put the batch's keys and values [tokens, heads, dim] (fp16 or bf16) into the cache, the keys turned by `rope` on the way.
         q [tokens, query heads, dim]: turned as well, into q_out (a new tensor if None), which is returned."""
-        import torch
-        device = _same_device("comet_cache_append", self.buf, batch.tensors[0], k, v, q, q_out, positions, status, None if rope is None else rope.steps)
-        tokens, dt = k.shape[0], k.dtype
-        rk = _rows3(k, "comet_cache_append: k", self.heads, self.dim)
-        rv = _rows3(v, "comet_cache_append: v", self.heads, self.dim, tokens, dt)
-        if positions is not None:
-            _int32(positions, "comet_cache_append: positions", tokens)
-        if q is None and q_out is not None:
+        dev = self._same("comet_cache_append", batch, rope)
+        on = _elsewhere(dev, stream)
+        if on is not None:
+            with on:
+                return self.comet_cache_append(batch, k, v, rope, q, q_out, positions, status)
+        tokens, dt, dim = k.shape[0], k.dtype, self.dim
+        rk = _rows3(k, "comet_cache_append: k", dev, tokens, self.heads, dim, dt)
+        rv = _rows3(v, "comet_cache_append: v", dev, tokens, self.heads, dim, dt)
+        if q is not None:
+            rq = _rows3(q, "comet_cache_append: q", dev, tokens, None, dim, dt)
+            q_heads = q.shape[1]
+            if q_out is None:
+                q_out = q.new_empty((tokens, q_heads, dim))
+            ro = _rows3(q_out, "comet_cache_append: q_out", dev, tokens, q_heads, dim, dt)
+        elif q_out is None:
+            q_heads, rq = 0, CacheRows()
+            ro = rq
+        else:
             raise ValueError("comet_cache_append: q_out without q")
-        with _On(device, stream) as st:
-            q_heads, rq, ro = 0, CacheRows(), CacheRows()
-            if q is not None:
-                rq = _rows3(q, "comet_cache_append: q", None, self.dim, tokens, dt)
-                q_heads = q.shape[1]
-                if q_out is None:
-                    q_out = torch.empty(q.shape, dtype=dt, device=device)
-                ro = _rows3(q_out, "comet_cache_append: q_out", q_heads, self.dim, tokens, dt)
-            _chk(lib().comet_cache_append(self._p, self.shape, C.byref(batch._c), tokens, rk, rv, rq, ro, q_heads, _dtype16(k),
-                                          None if rope is None else C.byref(rope._plan), None if positions is None else positions.data_ptr(), st,
-                                          _status_ptr(status)), "comet_cache_append")
+        pos = None if positions is None else _int32(positions, "comet_cache_append: positions", dev, tokens)
+        _chk(lib().comet_cache_append(self._p, self.shape, batch._c, tokens, rk, rv, rq, ro, q_heads, _dtype16(k), None if rope is None else rope._plan,
+                                      pos, _raw_stream(dev), _status_ptr(status, dev)), "comet_cache_append")
         return q_out
 
     def comet_cache_fetch(self, batch: Batch, k=None, v=None, dtype=None, tokens: int | None = None, status=None, stream=None):
         """The batch's keys and values as the cache holds them, (k, v): into the tensors given, or new ones of `dtype` with `tokens` rows (those
         that belong to no sequence stay as the allocator left them)."""
         import torch
-        device = _same_device("comet_cache_fetch", self.buf, batch.tensors[0], k, v, status)
-        with _On(device, stream) as st:
-            if k is None or v is None:
-                if tokens is None:
-                    tokens = (v if k is None else k).shape[0]
-                if dtype is None:
-                    dtype = (v if k is None else k).dtype
-                k = torch.empty((tokens, self.heads, self.dim), dtype=dtype, device=device) if k is None else k
-                v = torch.empty((tokens, self.heads, self.dim), dtype=dtype, device=device) if v is None else v
-            rk = _rows3(k, "comet_cache_fetch: k", self.heads, self.dim, tokens, dtype)
-            rv = _rows3(v, "comet_cache_fetch: v", self.heads, self.dim, k.shape[0], k.dtype)
-            _chk(lib().comet_cache_fetch(self._p, self.shape, C.byref(batch._c), k.shape[0], rk, rv, _dtype16(k), st, _status_ptr(status)),
-                 "comet_cache_fetch")
+        dev = self._same("comet_cache_fetch", batch)
+        on = _elsewhere(dev, stream)
+        if on is not None:
+            with on:
+                return self.comet_cache_fetch(batch, k, v, dtype, tokens, status)
+        given = v if k is None else k
+        if given is not None:
+            tokens = given.shape[0] if tokens is None else tokens
+            dtype = given.dtype if dtype is None else dtype
+        if tokens is None or dtype is None:
+            raise ValueError("comet_cache_fetch: tokens and dtype, or tensors for the result, expected")
+        if k is None:
+            k = torch.empty((tokens, self.heads, self.dim), dtype=dtype, device=self.buf.device)
+        if v is None:
+            v = torch.empty((tokens, self.heads, self.dim), dtype=dtype, device=self.buf.device)
+        rk = _rows3(k, "comet_cache_fetch: k", dev, tokens, self.heads, self.dim, dtype)
+        rv = _rows3(v, "comet_cache_fetch: v", dev, tokens, self.heads, self.dim, dtype)
+        _chk(lib().comet_cache_fetch(self._p, self.shape, batch._c, tokens, rk, rv, _dtype16(k), _raw_stream(dev), _status_ptr(status, dev)),
+             "comet_cache_fetch")
         return k, v
 
     def comet_cache_attend(self, batch: Batch, q, out=None, lse=None, scale: float | None = None, causal: bool = True, work=None, status=None,
@@ -559,27 +563,32 @@ class Cache:
         [tokens, query heads] for the log-sum-exp of every row, or True for a new one; then (out, lse) is returned, else out.  work: uint8 tensor
         of comet_cache_attend_work bytes, allocated if None."""
         import torch
-        device = _same_device("comet_cache_attend", self.buf, batch.tensors[0], q, out, None if lse is True else lse, work, status)
-        rq = _rows3(q, "comet_cache_attend: q", None, self.dim)
-        tokens, q_heads = q.shape[0], q.shape[1]
-        need = int(lib().comet_cache_attend_work(self.shape, batch.n_seqs, tokens, q_heads))
-        if not need:
-            raise CometError(ERR_INVALID, "comet_cache_attend_work")
-        with _On(device, stream) as st:
-            if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=device)
-            ro = _rows3(out, "comet_cache_attend: out", q_heads, self.dim, tokens, q.dtype)
-            if lse is True:
-                lse = torch.empty((tokens, q_heads), dtype=torch.float32, device=device)
-            elif lse is not None and (str(lse.dtype) != "torch.float32" or not lse.is_contiguous() or tuple(lse.shape) != (tokens, q_heads)):
-                raise ValueError("comet_cache_attend: lse: contiguous float32 tensor [tokens, query heads] expected")
-            if work is None:
-                work = torch.empty(need, dtype=torch.uint8, device=device)
-            elif not work.is_contiguous():
-                raise ValueError("comet_cache_attend: work: contiguous tensor expected")
-            _chk(lib().comet_cache_attend(self._p, self.shape, C.byref(batch._c), tokens, rq, q_heads, _dtype16(q),
-                                          self.dim ** -0.5 if scale is None else scale, 1 if causal else 0, ro, None if lse is None else lse.data_ptr(),
-                                          work.data_ptr(), work.numel() * work.element_size(), st, _status_ptr(status)), "comet_cache_attend")
+        dev = self._same("comet_cache_attend", batch)
+        on = _elsewhere(dev, stream)
+        if on is not None:
+            with on:
+                return self.comet_cache_attend(batch, q, out, lse, scale, causal, work, status)
+        tokens, dt, dim = q.shape[0], q.dtype, self.dim
+        rq = _rows3(q, "comet_cache_attend: q", dev, tokens, None, dim, dt)
+        q_heads = q.shape[1]
+        if out is None:
+            out = q.new_empty((tokens, q_heads, dim))
+        ro = _rows3(out, "comet_cache_attend: out", dev, tokens, q_heads, dim, dt)
+        if lse is True:
+            lse = q.new_empty((tokens, q_heads), dtype=torch.float32)
+        elif lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (tokens, q_heads) or lse.get_device() != dev):
+            raise ValueError("comet_cache_attend: lse: contiguous float32 tensor [tokens, query heads] on the device of the others expected")
+        L = lib()
+        if work is None:
+            need = L.comet_cache_attend_work(self.shape, batch.n_seqs, tokens, q_heads)
+            if not need:
+                raise CometError(ERR_INVALID, "comet_cache_attend_work")
+            work = torch.empty(need, dtype=torch.uint8, device=q.device)
+        elif not work.is_contiguous() or work.get_device() != dev:
+            raise ValueError("comet_cache_attend: work: contiguous tensor on the device of the others expected")
+        _chk(L.comet_cache_attend(self._p, self.shape, batch._c, tokens, rq, q_heads, _dtype16(q), dim ** -0.5 if scale is None else scale,
+                                  1 if causal else 0, ro, None if lse is None else lse.data_ptr(), work.data_ptr(),
+                                  work.numel() * work.element_size(), _raw_stream(dev), _status_ptr(status, dev)), "comet_cache_attend")
         return out if lse is None else (out, lse)
 
 

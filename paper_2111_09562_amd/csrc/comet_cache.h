@@ -91,16 +91,21 @@ struct AttendArgs {
     Rows q, out;
     float *lse;                               // [token][query head], or null
     uint32_t q_heads, group;                  // group: query heads of a key/value head
-    uint32_t bf16, causal, vec;
+    uint32_t bf16, causal, vec, wide;         // wide: k_attend_tile
+    uint32_t tile_rows, tile_shift;           // rows of a workgroup: 2^tile_shift
+    uint32_t min_blocks;                      // of a piece
     uint32_t pieces;                          // pieces the work of a key/value head is cut into, about
     uint32_t slots;                           // pieces there are at most
     float scale;                              // of the scores, times log2(e)
-    float *part_o;                            // [slot][32][dim]
-    float *part_s;                            // [slot][32][3]: maximum, sum, reference of the accumulated values
+    float *part_o;                            // [slot][head][tile_rows][dim]
+    float *part_s;                            // [slot][head][tile_rows][3]: reference and sum of the weights, reference of the values
     int32_t *directory;                       // [tile][2]: first piece, number of pieces
 };
 template <int NC>
 __global__ void k_attend(AttendArgs a);
+constexpr int attend_tile_rt(int nc) { return nc <= 4 ? 2 : 1; }      // tiles of 32 rows per wavefront: what fits its registers
+template <int NC, int RT>
+__global__ void k_attend_tile(AttendArgs a);
 __global__ void k_attend_join(AttendArgs a);
 
 // ---- types ------------------------------------------------------------------------------------------------------
@@ -202,19 +207,19 @@ __device__ inline void raise(int32_t *status) {
     if (status && lane_id() == 0) *status = COMET_ERR_FORMAT;
 }
 
-// Sequence b's units of `tokens * mul / div` are numbered from first_unit(b) on: at least as many numbers as it can need,
-// whatever the lengths, and known without adding up those in front of it.  With `extra` = 2 there is room for the blocks of 32 that n tokens
-// touch (div 32, mul 1), with 1 for tiles of 32 rows that begin with the sequence.
-__device__ inline uint32_t first_unit(const int32_t *starts, uint32_t b, uint32_t mul, uint32_t extra) {
-    return (uint32_t)(((uint64_t)(uint32_t)starts[b] * mul) >> 5) + extra * b;
+// Sequence b's units of 2^shift of its tokens * mul are numbered from first_unit(b) on: at least as many numbers as it can need,
+// whatever the lengths, and known without adding up those in front of it.  With `extra` = 2 there is room for the blocks of 32 that its
+// tokens touch (shift 5, mul 1), with 1 for tiles that begin with the sequence.
+__device__ inline uint32_t first_unit(const int32_t *starts, uint32_t b, uint32_t mul, uint32_t shift, uint32_t extra) {
+    return (uint32_t)(((uint64_t)(uint32_t)starts[b] * mul) >> shift) + extra * b;
 }
 // The last sequence whose units begin at or before `unit`, by all lanes of a wavefront: 64 candidates a turn.  Starts
 // that do not grow give some sequence, never one out of range.
-__device__ inline uint32_t find_sequence(const int32_t *starts, uint32_t n_seqs, uint32_t unit, uint32_t mul, uint32_t extra) {
+__device__ inline uint32_t find_sequence(const int32_t *starts, uint32_t n_seqs, uint32_t unit, uint32_t mul, uint32_t shift, uint32_t extra) {
     uint32_t lo = 0, len = n_seqs;
     while (len > 1u) {
         const uint32_t stride = (len + 63u) / 64u, off = (uint32_t)lane_id() * stride;
-        const bool le = off < len && first_unit(starts, lo + off, mul, extra) <= unit;
+        const bool le = off < len && first_unit(starts, lo + off, mul, shift, extra) <= unit;
         const uint32_t n = (uint32_t)__popcll(wave_ballot(le));
         const uint32_t k = n > 0u ? n - 1u : 0u;
         lo += k * stride;

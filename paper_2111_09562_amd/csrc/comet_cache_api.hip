@@ -87,24 +87,35 @@ void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tok
     k_rope<T, V><<<wg, kRopeBlock, 0, st>>>(r, g, x, y, n_tokens, heads, dim, sign);
 }
 
-constexpr uint32_t kAttendPieces = 1024;                 // workgroups an attention call is cut into, about
+constexpr uint32_t kAttendPieces = 1024, kAttendTilePieces = 256;     // workgroups an attention call is cut into, about
 struct AttendPlan {
-    uint32_t pieces, slots, tiles;
+    uint32_t pieces, slots, tiles, tile_shift, min_blocks;
+    bool wide;                                           // k_attend_tile
     uint64_t off_s, off_dir, bytes;
 };
 bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads, AttendPlan *p) {
     if (!valid_shape(s) || !q_heads || q_heads > kMaxQueryHeads || q_heads % s.heads || n_seqs > kMaxSeqs) return false;
     const uint64_t rows = (uint64_t)n_tokens * (q_heads / s.heads);
     if (rows > kMaxRows) return false;
-    p->tiles = (uint32_t)(rows / 32u) + n_seqs;
-    p->pieces = (kAttendPieces + s.heads - 1u) / s.heads;
-    p->slots = p->pieces + p->tiles;
-    const uint64_t n = (uint64_t)p->slots * s.heads;
+    p->wide = rows > 64ull * n_seqs;
+    p->tile_shift = !p->wide ? 5u : attend_tile_rt((int)s.dim / 32) == 2 ? 8u : 7u;
+    p->tiles = (uint32_t)(rows >> p->tile_shift) + n_seqs;
+    p->pieces = ((p->wide ? kAttendTilePieces : kAttendPieces) + s.heads - 1u) / s.heads;
+    p->min_blocks = p->wide ? 16u : 4u;
+    // a tile's pieces are counted as if it saw all of its sequence: of tiles of a causal prompt up to half have nothing to do
+    p->slots = (p->wide ? 2u : 1u) * p->pieces + p->tiles;
+    const uint64_t n = (uint64_t)p->slots * s.heads, per = 1ull << p->tile_shift;
     if (n > kMaxRows) return false;
-    p->off_s = n * 32u * s.dim * 4u;
-    p->off_dir = p->off_s + n * 32u * 3u * 4u;
+    p->off_s = n * per * s.dim * 4u;
+    p->off_dir = p->off_s + n * per * 3u * 4u;
     p->bytes = p->off_dir + 8ull * (p->tiles + 1ull);
     return true;
+}
+
+template <int NC>
+void launch_attend(const AttendArgs &a, bool wide, uint32_t wg, hipStream_t st) {
+    if (wide) k_attend_tile<NC, attend_tile_rt(NC)><<<wg, kAttendBlock, 0, st>>>(a);
+    else k_attend<NC><<<wg, kAttendBlock, 0, st>>>(a);
 }
 
 }  // namespace
@@ -230,8 +241,9 @@ int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const com
     if (!rows_args(q, dtype, &a.q) || !rows_args(out, dtype, &a.out) || !dev_work || (uintptr_t)dev_work % 16u) return COMET_ERR_INVALID;
     if (work_bytes < p.bytes) return COMET_ERR_NOMEM;
     a.lse = dev_lse; a.q_heads = q_heads; a.group = q_heads / shape.heads;
-    a.bf16 = dtype == COMET_BF16; a.causal = causal != 0; a.vec = rows_aligned(a.q, dtype) && rows_aligned(a.out, dtype);
-    a.pieces = p.pieces; a.slots = p.slots; a.scale = scale * 1.4426950408889634f;
+    a.bf16 = dtype == COMET_BF16; a.causal = causal != 0; a.wide = p.wide; a.vec = rows_aligned(a.q, dtype) && rows_aligned(a.out, dtype);
+    a.pieces = p.pieces; a.slots = p.slots; a.min_blocks = p.min_blocks; a.tile_shift = p.tile_shift; a.tile_rows = 1u << p.tile_shift;
+    a.scale = scale * 1.4426950408889634f;
     uint8_t *w = static_cast<uint8_t *>(dev_work);
     a.part_o = reinterpret_cast<float *>(w);
     a.part_s = reinterpret_cast<float *>(w + p.off_s);
@@ -239,17 +251,21 @@ int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const com
     hipStream_t st = (hipStream_t)stream;
     const uint32_t wg = p.slots * shape.heads;
     switch (shape.dim / 32u) {
-        case 1: k_attend<1><<<wg, kAttendBlock, 0, st>>>(a); break;
-        case 2: k_attend<2><<<wg, kAttendBlock, 0, st>>>(a); break;
-        case 3: k_attend<3><<<wg, kAttendBlock, 0, st>>>(a); break;
-        case 4: k_attend<4><<<wg, kAttendBlock, 0, st>>>(a); break;
-        case 5: k_attend<5><<<wg, kAttendBlock, 0, st>>>(a); break;
-        case 6: k_attend<6><<<wg, kAttendBlock, 0, st>>>(a); break;
-        case 7: k_attend<7><<<wg, kAttendBlock, 0, st>>>(a); break;
-        default: k_attend<8><<<wg, kAttendBlock, 0, st>>>(a); break;
+        case 1: launch_attend<1>(a, p.wide, wg, st); break;
+        case 2: launch_attend<2>(a, p.wide, wg, st); break;
+        case 3: launch_attend<3>(a, p.wide, wg, st); break;
+        case 4: launch_attend<4>(a, p.wide, wg, st); break;
+        case 5: launch_attend<5>(a, p.wide, wg, st); break;
+        case 6: launch_attend<6>(a, p.wide, wg, st); break;
+        case 7: launch_attend<7>(a, p.wide, wg, st); break;
+        default: launch_attend<8>(a, p.wide, wg, st); break;
     }
     HIP_TRY(hipGetLastError());
-    k_attend_join<<<p.tiles * shape.heads, kAttendBlock, 0, st>>>(a);
+    // the rows of a tile side by side while there are few tiles
+    const uint32_t groups = p.tiles * shape.heads;
+    uint32_t side = 2048u / groups;
+    side = side < 1u ? 1u : (side > a.tile_rows ? a.tile_rows : side);
+    k_attend_join<<<dim3(groups, side), kAttendBlock, 0, st>>>(a);
     HIP_TRY(hipGetLastError());
     return COMET_OK;
 }

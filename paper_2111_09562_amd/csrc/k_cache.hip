@@ -80,10 +80,10 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
     extern __shared__ __align__(16) uint16_t s_rows[];
     __shared__ uint32_t s_amax[2][kBlk];
     const uint32_t tid = threadIdx.x, unit = blockIdx.x, dim = a.c.dim, pitch = dim + 8u;
-    const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, 1u, 2u);
+    const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, 1u, 5u, 2u);
     Seq s;
     if (!read_sequence(a.b, seq, &s)) return;
-    const uint32_t first = first_unit(a.b.starts, seq, 1u, 2u);
+    const uint32_t first = first_unit(a.b.starts, seq, 1u, 5u, 2u);
     if (unit < first) return;
     if (s.len < s.n) {
         raise(a.b.status);
@@ -240,10 +240,10 @@ template <typename T>
 __global__ __launch_bounds__(kCacheBlock) void k_cache_fetch(FetchArgs a) {
     extern __shared__ __align__(16) uint16_t s_rows[];
     const uint32_t tid = threadIdx.x, unit = blockIdx.x, head = blockIdx.y, dim = a.c.dim, pitch = dim + 8u;
-    const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, 1u, 2u);
+    const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, 1u, 5u, 2u);
     Seq s;
     if (!read_sequence(a.b, seq, &s)) return;
-    const uint32_t first = first_unit(a.b.starts, seq, 1u, 2u);
+    const uint32_t first = first_unit(a.b.starts, seq, 1u, 5u, 2u);
     if (unit < first) return;
     if (s.len < s.n) {
         raise(a.b.status);

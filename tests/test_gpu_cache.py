@@ -307,6 +307,65 @@ def test_attend(comet, dtype, heads, group, dim, new, causal):
     assert torch.equal(out2[:sum(new)], out[:sum(new)]) and torch.equal(lse2[:sum(new)], lse[:sum(new)])
 
 
+@pytest.mark.parametrize("dtype,heads,group,dim,held,new,causal", [
+    ("bf16", 2, 4, 128, [0, 0, 0], [300, 1, 130], True), ("fp16", 1, 1, 64, [0, 700, 33], [700, 200, 0], True), ("bf16", 1, 16, 32, [2500, 5], [40, 9], True),
+    ("fp16", 2, 3, 96, [100, 3000], [257, 64], False), ("bf16", 1, 5, 160, [64, 31], [100, 33], True), ("fp16", 1, 8, 192, [2000], [70], True),
+    ("bf16", 1, 2, 224, [500, 0], [129, 300], False), ("fp16", 2, 2, 256, [96, 1500], [256, 65], True), ("bf16", 3, 1, 128, [4000], [128], True)])
+def test_attend_many_rows(comet, dtype, heads, group, dim, held, new, causal):
+    """Prompts and pieces of prompts: tiles of rows, blocks that some of a tile's rows see, long ranges that are cut."""
+    s = Sequences(comet, DT[dtype], heads, dim, len(new), 4300, page=128, seed=dim + heads)
+    s.grow(held)
+    s.grow(new)
+    q = s.tokens(sum(new) + 1, heads * group) * 2
+    batch = s.batch(new)
+    out = torch.full_like(q, 5.0, device="cuda")
+    out, lse = s.cache.comet_cache_attend(batch, q.cuda(), out=out, lse=True, causal=causal, status=s.status)
+    check_attend(s, new, q, out, lse, causal)
+    assert (out[sum(new):] == 5).all() and s.ok()
+    out2, lse2 = s.cache.comet_cache_attend(batch, q.cuda(), lse=True, causal=causal)
+    assert torch.equal(out2[:sum(new)], out[:sum(new)]) and torch.equal(lse2[:sum(new)], lse[:sum(new)])
+    if causal:                                # fewer tokens held than queries: the first rows see nothing
+        lens = [n - n // 2 for n in new]
+        out, lse = s.cache.comet_cache_attend(s.batch(new, lens=lens), q.cuda(), lse=True)
+        full = [n % 32 == 0 for n in lens]    # (an open block of that length is not in the ring any more)
+        at = 0
+        for b, n in enumerate(new):
+            assert not out[at:at + n // 2].any() and (lse[at:at + n // 2] == -math.inf).all()
+            if full[b] and n:
+                one = Sequences.__new__(Sequences)
+                one.__dict__.update(s.__dict__, lens=lens)
+                k, v = one.held(b)
+                o, _, size, top = ref.attention(q[at:at + n], k, v, dim ** -0.5, True)
+                d = (dim + 8) * U32 * top
+                assert ((out[at:at + n].cpu().double() - o).abs() <= (u(torch.float16) + 2 * d + 2.0 ** -19) * size + u(s.dt) * o.abs() + 2.0 ** -24).all()
+            at += n
+
+
+def test_many_rows_and_missing_pages(comet):
+    """A page that is none in the middle of a prompt's cache, and a block of NaN: the same values as with few rows at a time, where every call
+    goes another way through the library."""
+    s = Sequences(comet, torch.bfloat16, 1, 64, 1, 1024, seed=14)
+    k, v = s.tokens(900, 1), s.tokens(900, 1)
+    v[777] = float("nan")
+    s.grow([900], k=k, v=v)
+    q = s.tokens(300, 4)
+    s.table[0, 5] = -1                                                    # tokens 320 .. 383
+    out, lse = s.cache.comet_cache_attend(s.batch([300]), q.cuda(), lse=True, status=s.status)
+    assert int(s.status.item()) == comet.ERR_FORMAT
+    k, v = ref.held(s.cache, s.table.clamp_min(0), s.lens, s.slots, 0)
+    keep = torch.ones(900, dtype=torch.bool)
+    keep[320:384] = False
+    for i in (0, 100, 167, 168, 250, 299):
+        seen = keep[:601 + i]
+        o, want, size, top = ref.attention(q[i:i + 1], k[:, :601 + i][:, seen], v[:, :601 + i][:, seen], 0.125, False)
+        d = 72 * U32 * top
+        assert ((lse[i].cpu().double() - want).abs() <= d + 2.0 ** -18).all()
+        if 601 + i > 768:
+            assert out[i].isnan().all()
+        else:
+            assert ((out[i].cpu().double() - o).abs() <= (u(torch.float16) + 2 * d + 2.0 ** -19) * size + u(s.dt) * o.abs()).all()
+
+
 @pytest.mark.parametrize("lens,new", [([1], [1]), ([32], [1]), ([33], [33]), ([31, 1, 64], [31, 1, 2]), ([0, 5, 0], [2, 3, 0]), ([3, 40], [9, 50])])
 @pytest.mark.parametrize("causal", [True, False])
 def test_attend_short(comet, lens, new, causal):
@@ -387,7 +446,9 @@ def test_inf_and_nan(comet):
         first = where // 32 * 32 if where < 64 else where                 # the open block's tokens have scales of their own
         assert torch.equal(out[:first], want[:first]) and torch.equal(out[70:], want[70:]) and torch.equal(lse[:first], want_lse[:first])
         assert out[first:70].isnan().all()
-        assert torch.equal(lse[first:70, :2], want_lse[first:70, :2]) and lse[first:70, 2:].isnan().all()     # the values' NaN is no score's
+        # The values' NaN is no score's.  (Poisoned blocks take the way of blocks that not all rows see, which rounds in another order: each of both
+        # is off by at most (dim + 8) u(float32) times sum |q k| scale, here below 32, and 2^-20 of the sum's logarithm, here below 7.)
+        assert ((lse[first:70, :2] - want_lse[first:70, :2]).abs() <= 2 * (72 * U32 * 32 + 2.0 ** -20 * 8)).all() and lse[first:70, 2:].isnan().all()
         fk, fv = s.cache.comet_cache_fetch(s.batch([70, 20]), dtype=torch.bfloat16, tokens=90)
         end = min(70, first + 32) if where < 64 else where + 1
         assert fv[first:end, 0].isnan().all() and fk[first:end, 1].isnan().all()

@@ -22,6 +22,9 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
+# The attention kernels' accumulators stay in vector registers, where the vector instructions that scale and read them can reach them;
+# by default a kernel of one wavefront per SIMD has them in accumulation registers, a copy each way per use.
+UNIT_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for name in ("k_attend.hip", "k_attend_tile.hip")}
 OBJ = os.path.join(HERE, "_build")                   # object files (not tracked)
 JOBS = 8
 
@@ -37,7 +40,7 @@ def units():
     """The translation units: every .hip file.  No kernel calls device code of another unit, so
     no relocatable device code is needed; the longest units come first."""
     names = sorted(f for f in os.listdir(CSRC) if f.endswith(".hip"))
-    names.sort(key=lambda f: (not f.startswith("k_decompress"), not f.startswith("k_quantize_rows")))
+    names.sort(key=lambda f: (not f.startswith(("k_decompress", "k_attend")), not f.startswith("k_quantize_rows")))
     return [os.path.join(CSRC, f) for f in names]
 
 
@@ -56,7 +59,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         obj = os.path.join(OBJ, os.path.basename(src)[:-4] + ".o")
         objs.append(obj)
         if force or not os.path.exists(obj) or os.path.getmtime(obj) < max(os.path.getmtime(src), newest_header):
-            todo.append([cc] + FLAGS + ["-c", src, "-o", obj])
+            todo.append([cc] + FLAGS + UNIT_FLAGS.get(os.path.basename(src), []) + ["-c", src, "-o", obj])
     running = []
     def reap(block_until_below):
         while len(running) > block_until_below:

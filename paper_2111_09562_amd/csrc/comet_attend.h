@@ -1,0 +1,393 @@
+// Attention of the batch's queries over the compressed cache.
+//
+// One pass over the keys with a reference m near the running maximum and the sum l of every row.  With q the row, K and V the whole
+// numbers of a block and a, b its scales:  x = (q . K) a c,  p = exp2(x - r + log2 b + lift),  O += p V,  l += exp2(x - m),
+// o = O exp2(r - m - lift) / l.  r is a second reference, near the largest x + log2 b: p, which the matrix instruction takes in float16, is
+// then at most 2^15 whatever the scales of the blocks are, and weights down to 2^-21 of the largest keep all bits float16 has, down to 2^-32 some
+// (a hundred thousand tokens of next to no weight still count).  m and r move only once something exceeds them by 2^8: O
+// is hardly ever rescaled.  The whole numbers are exact in float16, so the only rounding below 32 bits is that of p, at most
+// 2^-11 of each weight.  The query goes in as float16 times a power of two of its row, which is exact for both 16-bit types but for
+// values below 2^-38 of the row's largest.
+#pragma once
+#include "comet_cache.h"
+#include "comet_scan.h"
+
+namespace comet {
+
+namespace {
+
+constexpr float kNegInf = -__builtin_inff();
+constexpr float kLift = 7.0f, kSlack = 8.0f;      // log2: weights are at most 2^(kLift + kSlack) on their way into float16
+
+// Tiles of a.tile_rows rows and blocks of a sequence.
+__device__ inline uint32_t tiles_of(const AttendArgs &a, uint32_t seq) {
+    const int32_t s0 = a.b.starts[seq], s1 = a.b.starts[seq + 1];
+    if (s0 < 0 || s1 <= s0 || s1 > (int32_t)a.b.n_tokens || a.b.lens[seq] < 0 || a.b.lens[seq] > kMaxLen) return 0u;
+    return (uint32_t)(((uint64_t)(uint32_t)(s1 - s0) * a.group + a.tile_rows - 1u) >> a.tile_shift);
+}
+__device__ inline uint32_t blocks_of(const AttendArgs &a, uint32_t seq) { return (uint32_t)((a.b.lens[seq] + 31ll) / 32); }
+
+__device__ inline uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+// Sum over the wavefront, the same in every lane.
+__device__ inline float wave_total(float v) {
+    const auto add = [](float x, int32_t y) { return x + __int_as_float(y); };
+    v = add(v, dpp0<0x111, 0xf, true>(__float_as_int(v)));
+    v = add(v, dpp0<0x112, 0xf, true>(__float_as_int(v)));
+    v = add(v, dpp0<0x114, 0xf, true>(__float_as_int(v)));
+    v = add(v, dpp0<0x118, 0xf, true>(__float_as_int(v)));
+    v = add(v, dpp0<0x142, 0xa, false>(__float_as_int(v)));
+    v = add(v, dpp0<0x143, 0xc, false>(__float_as_int(v)));
+    return __uint_as_float(lane_value(__float_as_uint(v), kWave - 1));
+}
+
+constexpr uint32_t kSorted = 32;                   // sequences that are put in order
+
+struct Piece {
+    uint32_t seq, tile, part;
+    uint32_t per;                         // blocks of a part
+    uint32_t number;                      // among all pieces of a head
+};
+// Cuts the blocks of all tiles into pieces of the same length, so that sequences of very different lengths keep all compute units
+// busy, and finds the piece `number`.  Everything comes from the lengths on the device: the host does not know
+// them, and a captured call goes by what they are when it is replayed.  By the whole workgroup, a sequence per thread (a second
+// read for those beyond 256); ends the same way for all threads.
+__device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p) {
+    __shared__ float s_sum[kAttendBlock / kWave];
+    __shared__ uint32_t s_scan[kAttendBlock / kWave], s_found[3];
+    __shared__ uint32_t s_order[kSorted][3];
+    const uint32_t tid = threadIdx.x, wave = tid / kWave;
+    float total = 0.0f;                       // blocks of all tiles; the same sum in the same order in every workgroup
+    uint32_t tiles = 0, blocks = 0;
+    for (uint32_t b = tid; b < a.b.n_seqs; b += kAttendBlock) {
+        const uint32_t t = tiles_of(a, b), k = blocks_of(a, b);
+        float v = (float)k;
+        if (a.causal && a.wide && t) {                         // on the average a tile sees as much as its sequence's middle one
+            const float half = (float)(a.b.starts[b + 1] - a.b.starts[b]) * (1.0f / 64.0f);
+            v = fmaxf(v - half, v * 0.5f);                     // (never less than half: a.slots counts on it)
+        }
+        total += v * (float)t;
+        if (b == tid) {
+            tiles = t;
+            blocks = k;
+        }
+    }
+    total = wave_total(total);
+    if (lane_id() == 0) s_sum[wave] = total;
+    if (tid == 0u) s_found[0] = 0xffffffffu;
+    __syncthreads();
+    total = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+    // an eighth more than the average (a tile that is just longer than that is not worth a second piece), which also keeps what float32
+    // rounds from making more pieces than there are slots
+    const float most = __builtin_ceilf(total * 1.125f / (float)a.pieces);
+    uint32_t per = most < 2147483000.0f ? (uint32_t)most : 2147483000u;
+    if (per < a.min_blocks) per = a.min_blocks;
+    // A few prompts: the longest sequences first, so that no long tile begins when the others are done.
+    uint32_t whose = tid;
+    const bool sorted = a.wide && a.b.n_seqs > 1u && a.b.n_seqs <= kSorted;
+    if (sorted) {
+        if (wave == 0u) {
+            uint32_t rank = 0;
+            for (uint32_t k = 0; k < a.b.n_seqs; ++k) {
+                const uint32_t other = lane_value(blocks, (int)k);
+                rank += other > blocks || (other == blocks && k < tid);
+            }
+            if (tid < a.b.n_seqs) {
+                s_order[rank][0] = tid;
+                s_order[rank][1] = tiles;
+                s_order[rank][2] = blocks;
+            }
+        }
+        __syncthreads();
+        if (tid < a.b.n_seqs) {
+            whose = s_order[tid][0];
+            tiles = s_order[tid][1];
+            blocks = s_order[tid][2];
+        }
+    }
+    uint32_t base = 0;
+    for (uint32_t b0 = 0; b0 < a.b.n_seqs && base <= number; b0 += kAttendBlock) {
+        const uint32_t b = b0 + tid;
+        if (b0) {
+            tiles = b < a.b.n_seqs ? tiles_of(a, b) : 0u;
+            blocks = b < a.b.n_seqs ? blocks_of(a, b) : 0u;
+        }
+        const uint32_t parts = blocks > per ? (blocks + per - 1u) / per : 1u, count = tiles * parts;
+        const uint32_t incl = (uint32_t)run_scan<2>((int32_t)count, 0u, 64u);
+        if (lane_id() == kWave - 1) s_scan[wave] = incl;
+        __syncthreads();
+        uint32_t before = base + incl - count;
+#pragma unroll
+        for (uint32_t w = 0; w < kAttendBlock / kWave; ++w) {
+            if (w < wave) before += s_scan[w];
+            base += s_scan[w];
+        }
+        if (number - before < count) {
+            const uint32_t local = number - before, tile = local / parts;
+            if (tile < tiles) {                                // (not so only where the batch's numbers make no sense)
+                s_found[0] = sorted ? whose : b;
+                s_found[1] = a.causal ? tiles - 1u - tile : tile;      // a causal prompt's last tiles see most: they begin first
+                s_found[2] = local - tile * parts;
+            }
+        }
+        __syncthreads();
+    }
+    p->seq = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_found[0]);
+    p->tile = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_found[1]);
+    p->part = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_found[2]);
+    p->per = (uint32_t)__builtin_amdgcn_readfirstlane((int)per);
+    p->number = number;
+    return p->seq != 0xffffffffu;
+}
+
+// Eight whole numbers of 8 bits as float16: a byte u = v + 128 behind the byte 0x64 is the float16 number 1024 + u.
+__device__ inline half8 whole8(uint32_t lo, uint32_t hi) {
+    lo ^= 0x80808080u;
+    hi ^= 0x80808080u;
+    const uint32_t m = 0x64646464u;
+    const half2v off = {(_Float16)1152.0f, (_Float16)1152.0f};
+    const half2v a = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(m, lo, 0x04010400u)) - off;
+    const half2v b = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(m, lo, 0x04030402u)) - off;
+    const half2v c = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(m, hi, 0x04010400u)) - off;
+    const half2v d = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(m, hi, 0x04030402u)) - off;
+    return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The other half of the wavefront's value for the same row.
+__device__ inline float other_half(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(lane_id() < 32 ? r[1] : r[0]);
+}
+__device__ inline float other_half_max(float v) { return fmaxf(v, other_half(v)); }
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
+
+// A row's numbers: lane l has those of row l & 31, the accumulated values 32c + 8 * (i / 4) + 4 * (l >> 5) + i % 4 of it.
+template <int NC>
+struct RowState {
+    f32x16 o[NC];
+    float m, r, l;              // l: of the lane's own tokens until the end
+    __device__ void clear() {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[c] = f32x16{};
+        m = r = kNegInf;
+        l = 0.0f;
+    }
+    // top: the largest x of the row's new tokens, tope: of x + log2 b
+    __device__ void follow(float top, float tope) {
+        if (wave_ballot(top > m + kSlack || tope > r + kSlack || (m == kNegInf && top > kNegInf))) {
+            const float m2 = fmaxf(m, top), r2 = fmaxf(r, tope);
+            const float alpha = exp2_fast(r - (r2 == kNegInf ? 0.0f : r2));
+            l *= exp2_fast(m - (m2 == kNegInf ? 0.0f : m2));
+#pragma unroll
+            for (int c = 0; c < NC; ++c) o[c] *= alpha;
+            m = m2;
+            r = r2;
+        }
+    }
+    // The weights of a block that the whole tile sees, from its raw products; kc = a c, lb = log2 b.
+    __device__ void weights(const f32x16 &s, float kc, float lb, half8 *p) {
+        // where b is so small that p is 0 anyway, only l counts
+        const float c1 = fmaxf(lb - r + kLift, -60.0f - m);
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+            const float w = exp2_fast(__builtin_fmaf(s[t], kc, c1));
+            sum[t % 4] += w;
+            p[t / 8][t % 8] = (_Float16)w;
+        }
+        l = __builtin_fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), exp2_fast(-c1 - m), l);
+    }
+    // The same for a block of which rows see parts: x = -Inf elsewhere.  A poisoned block's lb is NaN, and so are the weights seen.
+    __device__ void weights_some(const float *x, float lb, half8 *p) {
+        const float ms = m == kNegInf ? 0.0f : m, c1 = lb - (r == kNegInf ? 0.0f : r) + kLift;
+        float sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+            sum += exp2_fast(x[t] - ms);
+            p[t / 8][t % 8] = (_Float16)exp2_fast(x[t] + c1);
+        }
+        l += sum;
+        if (lb != lb) {
+#pragma unroll
+            for (int t = 0; t < 16; ++t)
+                if (x[t] == kNegInf) p[t / 8][t % 8] = (_Float16)0.0f;
+        }
+    }
+    // ... and for tokens each with a scale of its own: lv = log2 b, 0 where x = -Inf.
+    __device__ void weights_each(const float *x, const float *lv, half8 *p) {
+        const float ms = m == kNegInf ? 0.0f : m, rs = r == kNegInf ? 0.0f : r;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+            l += exp2_fast(x[t] - ms);
+            p[t / 8][t % 8] = (_Float16)exp2_fast(x[t] + (lv[t] - rs + kLift));
+        }
+    }
+};
+
+// What a row is: the query, where its values are and go, how many tokens it sees.
+struct RowPlace {
+    bool real;
+    uint32_t qh;
+    int64_t token;
+    int32_t limit;
+};
+__device__ inline RowPlace row_place(const AttendArgs &a, const Seq &s, uint32_t head, uint32_t row) {
+    RowPlace p;
+    const uint32_t rows = (uint32_t)s.n * a.group;
+    p.real = row < rows;
+    const uint32_t query = p.real ? row / a.group : (uint32_t)s.n - 1u;
+    p.qh = head * a.group + (p.real ? row - query * a.group : 0u);
+    p.token = (int64_t)s.start + query;
+    p.limit = a.causal ? s.len - s.n + (int32_t)query + 1 : s.len;
+    return p;
+}
+// tokens seen by the first and by the last of the rows row0 .. row0 + count - 1 (those that there are)
+__device__ inline void row_limits(const AttendArgs &a, const Seq &s, uint32_t row0, uint32_t count, int32_t *least, int32_t *most) {
+    const uint32_t rows = (uint32_t)s.n * a.group, last = row0 + count - 1u < rows ? row0 + count - 1u : rows - 1u;
+    *least = a.causal ? s.len - s.n + (int32_t)((row0 < rows ? row0 : rows - 1u) / a.group) + 1 : s.len;
+    *most = a.causal ? s.len - s.n + (int32_t)(last / a.group) + 1 : s.len;
+}
+
+// The row's query as the right operand: float16 times a power of two, which is returned.  Requested first, so that other loads can follow
+// before it is waited for.
+template <int NC>
+struct QueryRaw { uint32_t w[NC][8]; };
+template <int NC>
+__device__ inline void request_query(const AttendArgs &a, const RowPlace &p, QueryRaw<NC> *raw) {
+    const uint32_t h = (uint32_t)lane_id() >> 5;
+    const uint16_t *src = reinterpret_cast<const uint16_t *>(a.q.p) + p.token * a.q.token + (int64_t)p.qh * a.q.head;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const uint16_t *at = src + c * 32 + h * 16;
+        if (a.vec) {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(at), y = *reinterpret_cast<const u32x4 *>(at + 8);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { raw->w[c][i] = x[i]; raw->w[c][4 + i] = y[i]; }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) raw->w[c][i] = at[2 * i] | (uint32_t)at[2 * i + 1] << 16;
+        }
+    }
+}
+template <int NC>
+__device__ inline float convert_query(const AttendArgs &a, const QueryRaw<NC> &raw, half8 *q) {
+    if (!a.bf16) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const half2v two = __builtin_bit_cast(half2v, raw.w[c][i]);
+                q[2 * c + i / 4][2 * (i % 4)] = two[0];
+                q[2 * c + i / 4][2 * (i % 4) + 1] = two[1];
+            }
+        return 1.0f;
+    }
+    float top = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw.w[c][i] << 16)), fabsf(__uint_as_float(raw.w[c][i] & 0xffff0000u))));
+    top = other_half_max(top);
+    uint32_t e = __float_as_uint(top) >> 23;
+    e = e < 15u ? 15u : e;
+    const float scale = __uint_as_float((e - 14u) << 23);              // 2^(exponent - 14): the largest comes to lie in [2^14, 2^15)
+    const float inv = __uint_as_float((268u - e) << 23);               // 1 / scale (Inf in a row leaves Inf or NaN in it either way)
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            q[2 * c + i / 4][2 * (i % 4)] = (_Float16)(__uint_as_float(raw.w[c][i] << 16) * inv);
+            q[2 * c + i / 4][2 * (i % 4) + 1] = (_Float16)(__uint_as_float(raw.w[c][i] & 0xffff0000u) * inv);
+        }
+    return scale;
+}
+
+// Where a block lies and its scales: looked up by the lanes of a wavefront, one block each.
+struct Lookup {
+    int64_t index;              // or -1: no such page
+    float ks, lb;               // scale of the keys, log2 of the values'
+    __device__ void get(const AttendArgs &a, uint32_t seq, uint32_t head, uint32_t j, uint32_t end) {
+        index = -1;
+        ks = lb = 0.0f;
+        if (j < end) {
+            const uint32_t col = j / a.c.per;
+            const int32_t page = col < a.b.width ? a.b.table[(uint64_t)seq * a.b.width + col] : -1;
+            if (page >= 0 && (uint32_t)page < a.c.n_pages) {
+                index = ((int64_t)page * a.c.heads + head) * a.c.per + (j - col * a.c.per);
+                ks = a.c.scales[2 * index];
+                lb = log2_fast(a.c.scales[2 * index + 1]);
+            } else if (a.b.status) {
+                *a.b.status = COMET_ERR_FORMAT;
+            }
+        }
+    }
+    __device__ int64_t index_of(uint32_t i) const {
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(uint64_t)index, (int)i);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)index >> 32), (int)i);
+        return (int64_t)((uint64_t)hi << 32 | lo);
+    }
+    __device__ static float of(float v, uint32_t i) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), (int)i)); }
+};
+
+// x of a block's tokens from its raw products: visible are those before `limit`.
+__device__ inline void some_of_block(const f32x16 &s, float kc, float lb, uint32_t j, int32_t limit, float *x, float *top, float *tope) {
+    const int32_t left = limit - (int32_t)(j * 32u) - 4 * (int32_t)((uint32_t)lane_id() >> 5);
+    float best = kNegInf;
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+        const float v = s[t] * kc;
+        x[t] = 8 * (t / 4) + t % 4 < left ? v : kNegInf;
+        best = fmaxf(best, x[t]);
+    }
+    *top = other_half_max(best);
+    *tope = *top + lb;                        // (NaN for a poisoned block: no reference follows it)
+}
+// x and lv (weights_each) of the open block's tokens, with their own scales; `held` of its tokens are there.
+__device__ inline void each_of_open(const f32x16 &s, float qc, const float *ke, uint32_t held, uint32_t j, int32_t limit, float *x, float *lv, float *top, float *tope) {
+    const uint32_t h = (uint32_t)lane_id() >> 5;
+    float best = kNegInf, bests = kNegInf;
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+        const uint32_t tok = 8u * (t / 4) + 4u * h + t % 4;
+        const bool see = tok < held && (int32_t)(j * 32u + tok) < limit;
+        const float kt = ke[tok], vt = ke[32u + tok];
+        x[t] = see ? s[t] * (kt * qc) : kNegInf;
+        lv[t] = !see ? 0.0f : vt == vt ? (float)((int)(__float_as_uint(vt) >> 23) - 127) : vt;      // a power of two
+        best = fmaxf(best, x[t]);
+        bests = fmaxf(bests, x[t] + lv[t]);
+    }
+    *top = other_half_max(best);
+    *tope = other_half_max(bests);
+}
+// The open block's values as an operand: places nobody has written yet may hold anything.
+__device__ inline half8 open_values(const uint8_t *at, uint32_t u, uint32_t held) {
+    const uint32_t h = (uint32_t)lane_id() >> 5;
+    half8 v = *reinterpret_cast<const half8 *>(at);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (16u * u + 8u * (i / 4) + 4u * h + i % 4 >= held) v[i] = (_Float16)0.0f;
+    return v;
+}
+__device__ inline float log_sum(float m, float l) {                     // natural logarithm of l 2^m
+    return l > 0.0f ? (m + __log2f(l)) * 0.6931471805599453f : (l == l ? kNegInf : l);
+}
+__device__ inline f32x16 mfma(half8 a, half8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ inline void store_out(const AttendArgs &a, const RowPlace &p, uint32_t d, f32x4 v) {
+    uint16_t *dst = reinterpret_cast<uint16_t *>(a.out.p) + p.token * a.out.token + (int64_t)p.qh * a.out.head + d;
+    uint16_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = a.bf16 ? __builtin_bit_cast(uint16_t, (__bf16)v[i]) : __builtin_bit_cast(uint16_t, (_Float16)v[i]);
+    if (a.vec) {
+        *reinterpret_cast<uint2 *>(dst) = uint2{w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dst[i] = w[i];
+    }
+}
+// Parts of a tile that have something to do.
+__device__ inline uint32_t parts_of(uint32_t seen, uint32_t per) { return seen > per ? (seen + per - 1u) / per : 1u; }
+
+}  // namespace
+
+}  // namespace comet

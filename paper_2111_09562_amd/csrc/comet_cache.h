@@ -103,10 +103,10 @@ struct AttendArgs {
 };
 template <int NC>
 __global__ void k_attend(AttendArgs a);
-constexpr int attend_tile_rt(int nc) { return nc <= 4 ? 2 : 1; }      // tiles of 32 rows per wavefront: what fits its registers
 template <int NC, int RT>
 __global__ void k_attend_tile(AttendArgs a);
 __global__ void k_attend_join(AttendArgs a);
+__global__ void k_attend_join_tile(AttendArgs a);
 
 // ---- types ------------------------------------------------------------------------------------------------------
 using half8 = _Float16 __attribute__((ext_vector_type(8)));

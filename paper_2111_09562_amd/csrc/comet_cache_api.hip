@@ -87,10 +87,10 @@ void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tok
     k_rope<T, V><<<wg, kRopeBlock, 0, st>>>(r, g, x, y, n_tokens, heads, dim, sign);
 }
 
-constexpr uint32_t kAttendPieces = 1024, kAttendTilePieces = 256;     // workgroups an attention call is cut into, about
+constexpr uint32_t kAttendPieces = 768, kAttendTilePieces = 512;     // workgroups an attention call is cut into, about
 struct AttendPlan {
     uint32_t pieces, slots, tiles, tile_shift, min_blocks;
-    bool wide;                                           // k_attend_tile
+    bool wide, two;                                      // k_attend_tile; with two tiles of 32 rows per wavefront
     uint64_t off_s, off_dir, bytes;
 };
 bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads, AttendPlan *p) {
@@ -98,7 +98,10 @@ bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32
     const uint64_t rows = (uint64_t)n_tokens * (q_heads / s.heads);
     if (rows > kMaxRows) return false;
     p->wide = rows > 64ull * n_seqs;
-    p->tile_shift = !p->wide ? 5u : attend_tile_rt((int)s.dim / 32) == 2 ? 8u : 7u;
+    // Tiles of 256 rows for heads of up to 64, of 128 for those beyond 128 (what fits the registers); between, 256 rows once prompts are long:
+    // 8 x 4 heads of 128, prompts of 500 to 4096 tokens 137 us (128 rows: 123), 4096 tokens behind 28672 2.10 ms (2.26).
+    p->two = s.dim <= 64u || (s.dim <= 128u && n_tokens / 4096u >= n_seqs);
+    p->tile_shift = !p->wide ? 5u : p->two ? 8u : 7u;
     p->tiles = (uint32_t)(rows >> p->tile_shift) + n_seqs;
     p->pieces = ((p->wide ? kAttendTilePieces : kAttendPieces) + s.heads - 1u) / s.heads;
     p->min_blocks = p->wide ? 16u : 4u;
@@ -113,9 +116,18 @@ bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32
 }
 
 template <int NC>
-void launch_attend(const AttendArgs &a, bool wide, uint32_t wg, hipStream_t st) {
-    if (wide) k_attend_tile<NC, attend_tile_rt(NC)><<<wg, kAttendBlock, 0, st>>>(a);
-    else k_attend<NC><<<wg, kAttendBlock, 0, st>>>(a);
+void launch_attend(const AttendArgs &a, const AttendPlan &p, uint32_t wg, hipStream_t st) {
+    if constexpr (NC <= 4)
+        if (p.wide && p.two) {
+            k_attend_tile<NC, 2><<<wg, kAttendBlock, 0, st>>>(a);
+            return;
+        }
+    if constexpr (NC > 2)
+        if (p.wide) {
+            k_attend_tile<NC, 1><<<wg, kAttendBlock, 0, st>>>(a);
+            return;
+        }
+    k_attend<NC><<<wg, kAttendBlock, 0, st>>>(a);
 }
 
 }  // namespace
@@ -251,21 +263,24 @@ int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const com
     hipStream_t st = (hipStream_t)stream;
     const uint32_t wg = p.slots * shape.heads;
     switch (shape.dim / 32u) {
-        case 1: launch_attend<1>(a, p.wide, wg, st); break;
-        case 2: launch_attend<2>(a, p.wide, wg, st); break;
-        case 3: launch_attend<3>(a, p.wide, wg, st); break;
-        case 4: launch_attend<4>(a, p.wide, wg, st); break;
-        case 5: launch_attend<5>(a, p.wide, wg, st); break;
-        case 6: launch_attend<6>(a, p.wide, wg, st); break;
-        case 7: launch_attend<7>(a, p.wide, wg, st); break;
-        default: launch_attend<8>(a, p.wide, wg, st); break;
+        case 1: launch_attend<1>(a, p, wg, st); break;
+        case 2: launch_attend<2>(a, p, wg, st); break;
+        case 3: launch_attend<3>(a, p, wg, st); break;
+        case 4: launch_attend<4>(a, p, wg, st); break;
+        case 5: launch_attend<5>(a, p, wg, st); break;
+        case 6: launch_attend<6>(a, p, wg, st); break;
+        case 7: launch_attend<7>(a, p, wg, st); break;
+        default: launch_attend<8>(a, p, wg, st); break;
     }
     HIP_TRY(hipGetLastError());
-    // the rows of a tile side by side while there are few tiles
     const uint32_t groups = p.tiles * shape.heads;
-    uint32_t side = 2048u / groups;
-    side = side < 1u ? 1u : (side > a.tile_rows ? a.tile_rows : side);
-    k_attend_join<<<dim3(groups, side), kAttendBlock, 0, st>>>(a);
+    if (p.wide) {
+        k_attend_join_tile<<<dim3(groups, 8u), kAttendBlock, 0, st>>>(a);
+    } else {
+        uint32_t side = 2048u / groups;                  // the rows of a tile side by side while there are few tiles
+        side = side < 1u ? 1u : (side > a.tile_rows ? a.tile_rows : side);
+        k_attend_join<<<dim3(groups, side), kAttendBlock, 0, st>>>(a);
+    }
     HIP_TRY(hipGetLastError());
     return COMET_OK;
 }

@@ -21,8 +21,11 @@ constexpr float kLift = 7.0f, kSlack = 8.0f;      // log2: weights are at most 2
 
 // Tiles of a.tile_rows rows and blocks of a sequence.
 __device__ inline uint32_t tiles_of(const AttendArgs &a, uint32_t seq) {
-    const int32_t s0 = a.b.starts[seq], s1 = a.b.starts[seq + 1];
-    if (s0 < 0 || s1 <= s0 || s1 > (int32_t)a.b.n_tokens || a.b.lens[seq] < 0 || a.b.lens[seq] > kMaxLen) return 0u;
+    const int32_t s0 = a.b.starts[seq], s1 = a.b.starts[seq + 1], len = a.b.lens[seq];
+    if (s0 < 0 || s1 < s0 || s1 > (int32_t)a.b.n_tokens || len < 0 || len > kMaxLen) {
+        if (a.b.status) *a.b.status = COMET_ERR_FORMAT;
+        return 0u;
+    }
     return (uint32_t)(((uint64_t)(uint32_t)(s1 - s0) * a.group + a.tile_rows - 1u) >> a.tile_shift);
 }
 __device__ inline uint32_t blocks_of(const AttendArgs &a, uint32_t seq) { return (uint32_t)((a.b.lens[seq] + 31ll) / 32); }
@@ -46,6 +49,7 @@ struct Piece {
     uint32_t seq, tile, part;
     uint32_t per;                         // blocks of a part
     uint32_t number;                      // among all pieces of a head
+    Seq s;
 };
 // Cuts the blocks of all tiles into pieces of the same length, so that sequences of very different lengths keep all compute units
 // busy, and finds the piece `number`.  Everything comes from the lengths on the device: the host does not know
@@ -53,13 +57,13 @@ struct Piece {
 // read for those beyond 256); ends the same way for all threads.
 __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p) {
     __shared__ float s_sum[kAttendBlock / kWave];
-    __shared__ uint32_t s_scan[kAttendBlock / kWave], s_found[3];
+    __shared__ uint32_t s_scan[kAttendBlock / kWave], s_found[6];
     __shared__ uint32_t s_order[kSorted][3];
     const uint32_t tid = threadIdx.x, wave = tid / kWave;
     float total = 0.0f;                       // blocks of all tiles; the same sum in the same order in every workgroup
     uint32_t tiles = 0, blocks = 0;
     for (uint32_t b = tid; b < a.b.n_seqs; b += kAttendBlock) {
-        const uint32_t t = tiles_of(a, b), k = blocks_of(a, b);
+        const uint32_t t = tiles_of(a, b), k = t ? blocks_of(a, b) : 0u;
         float v = (float)k;
         if (a.causal && a.wide && t) {                         // on the average a tile sees as much as its sequence's middle one
             const float half = (float)(a.b.starts[b + 1] - a.b.starts[b]) * (1.0f / 64.0f);
@@ -109,7 +113,7 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
         const uint32_t b = b0 + tid;
         if (b0) {
             tiles = b < a.b.n_seqs ? tiles_of(a, b) : 0u;
-            blocks = b < a.b.n_seqs ? blocks_of(a, b) : 0u;
+            blocks = tiles ? blocks_of(a, b) : 0u;
         }
         const uint32_t parts = blocks > per ? (blocks + per - 1u) / per : 1u, count = tiles * parts;
         const uint32_t incl = (uint32_t)run_scan<2>((int32_t)count, 0u, 64u);
@@ -127,6 +131,10 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
                 s_found[0] = sorted ? whose : b;
                 s_found[1] = a.causal ? tiles - 1u - tile : tile;      // a causal prompt's last tiles see most: they begin first
                 s_found[2] = local - tile * parts;
+                const uint32_t seq = s_found[0];
+                s_found[3] = (uint32_t)a.b.starts[seq];
+                s_found[4] = (uint32_t)(a.b.starts[seq + 1] - a.b.starts[seq]);
+                s_found[5] = (uint32_t)a.b.lens[seq];
             }
         }
         __syncthreads();
@@ -136,7 +144,10 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
     p->part = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_found[2]);
     p->per = (uint32_t)__builtin_amdgcn_readfirstlane((int)per);
     p->number = number;
-    return p->seq != 0xffffffffu;
+    p->s.start = __builtin_amdgcn_readfirstlane((int)s_found[3]);
+    p->s.n = __builtin_amdgcn_readfirstlane((int)s_found[4]);
+    p->s.len = __builtin_amdgcn_readfirstlane((int)s_found[5]);
+    return p->seq != 0xffffffffu;             // (a sequence whose numbers make no sense has no tiles)
 }
 
 // Eight whole numbers of 8 bits as float16: a byte u = v + 128 behind the byte 0x64 is the float16 number 1024 + u.
@@ -152,23 +163,45 @@ __device__ inline half8 whole8(uint32_t lo, uint32_t hi) {
     return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// The other half of the wavefront's value for the same row.
-__device__ inline float other_half(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(lane_id() < 32 ? r[1] : r[0]);
+// Largest value and sum over the lanes of a row: l and l ^ 32, for tiles of 16 rows those that differ by a multiple of 16.
+template <int ROWS>
+__device__ inline float row_max(float v) {
+    if constexpr (ROWS == 16) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+    }
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
-__device__ inline float other_half_max(float v) { return fmaxf(v, other_half(v)); }
+template <int ROWS>
+__device__ inline float row_sum(float v) {
+    if constexpr (ROWS == 16) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
-// A row's numbers: lane l has those of row l & 31, the accumulated values 32c + 8 * (i / 4) + 4 * (l >> 5) + i % 4 of it.
-template <int NC>
+// Tiles of 32 or of 16 rows.  Which of a block's tokens lane l's score t is of, and where its values of the head are (ROWS registers of
+// 32 * 32 or 16 * 16 results): as the matrix instruction leaves them.
+template <int ROWS> constexpr int kScores = ROWS / 2;                    // scores of a lane per block
+template <int ROWS> __device__ inline uint32_t token_of(int t) {
+    if (ROWS == 32) return 8u * (t / 4) + 4u * ((uint32_t)lane_id() >> 5) + t % 4;
+    return 16u * (t / 4) + 4u * ((uint32_t)lane_id() >> 4) + t % 4;
+}
+
+// A row's numbers, in the lanes l with l % ROWS its number in the tile.
+template <int NO, typename ACC, int ROWS>
 struct RowState {
-    f32x16 o[NC];
+    static constexpr int N = kScores<ROWS>;
+    ACC o[NO];
     float m, r, l;              // l: of the lane's own tokens until the end
     __device__ void clear() {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) o[c] = f32x16{};
+        for (int c = 0; c < NO; ++c) o[c] = ACC{};
         m = r = kNegInf;
         l = 0.0f;
     }
@@ -179,18 +212,19 @@ struct RowState {
             const float alpha = exp2_fast(r - (r2 == kNegInf ? 0.0f : r2));
             l *= exp2_fast(m - (m2 == kNegInf ? 0.0f : m2));
 #pragma unroll
-            for (int c = 0; c < NC; ++c) o[c] *= alpha;
+            for (int c = 0; c < NO; ++c) o[c] *= alpha;
             m = m2;
             r = r2;
         }
     }
     // The weights of a block that the whole tile sees, from its raw products; kc = a c, lb = log2 b.
-    __device__ void weights(const f32x16 &s, float kc, float lb, half8 *p) {
+    template <typename S>
+    __device__ void weights(const S &s, float kc, float lb, half8 *p) {
         // where b is so small that p is 0 anyway, only l counts
         const float c1 = fmaxf(lb - r + kLift, -60.0f - m);
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
+        for (int t = 0; t < N; ++t) {
             const float w = exp2_fast(__builtin_fmaf(s[t], kc, c1));
             sum[t % 4] += w;
             p[t / 8][t % 8] = (_Float16)w;
@@ -202,14 +236,14 @@ struct RowState {
         const float ms = m == kNegInf ? 0.0f : m, c1 = lb - (r == kNegInf ? 0.0f : r) + kLift;
         float sum = 0.0f;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
+        for (int t = 0; t < N; ++t) {
             sum += exp2_fast(x[t] - ms);
             p[t / 8][t % 8] = (_Float16)exp2_fast(x[t] + c1);
         }
         l += sum;
         if (lb != lb) {
 #pragma unroll
-            for (int t = 0; t < 16; ++t)
+            for (int t = 0; t < N; ++t)
                 if (x[t] == kNegInf) p[t / 8][t % 8] = (_Float16)0.0f;
         }
     }
@@ -217,7 +251,7 @@ struct RowState {
     __device__ void weights_each(const float *x, const float *lv, half8 *p) {
         const float ms = m == kNegInf ? 0.0f : m, rs = r == kNegInf ? 0.0f : r;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
+        for (int t = 0; t < N; ++t) {
             l += exp2_fast(x[t] - ms);
             p[t / 8][t % 8] = (_Float16)exp2_fast(x[t] + (lv[t] - rs + kLift));
         }
@@ -250,56 +284,52 @@ __device__ inline void row_limits(const AttendArgs &a, const Seq &s, uint32_t ro
 
 // The row's query as the right operand: float16 times a power of two, which is returned.  Requested first, so that other loads can follow
 // before it is waited for.
-template <int NC>
-struct QueryRaw { uint32_t w[NC][8]; };
-template <int NC>
-__device__ inline void request_query(const AttendArgs &a, const RowPlace &p, QueryRaw<NC> *raw) {
-    const uint32_t h = (uint32_t)lane_id() >> 5;
-    const uint16_t *src = reinterpret_cast<const uint16_t *>(a.q.p) + p.token * a.q.token + (int64_t)p.qh * a.q.head;
+template <int NW>
+struct QueryRaw { uint32_t w[NW]; };             // pairs of 16-bit values, in the order of the operand
+// COUNT values from every 32nd of the head on, `at` of them behind it.
+template <int NC, int COUNT>
+__device__ inline void request_query(const AttendArgs &a, const RowPlace &p, uint32_t at, QueryRaw<NC * COUNT / 2> *raw) {
+    const uint16_t *src = reinterpret_cast<const uint16_t *>(a.q.p) + p.token * a.q.token + (int64_t)p.qh * a.q.head + at;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const uint16_t *at = src + c * 32 + h * 16;
         if (a.vec) {
-            const u32x4 x = *reinterpret_cast<const u32x4 *>(at), y = *reinterpret_cast<const u32x4 *>(at + 8);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { raw->w[c][i] = x[i]; raw->w[c][4 + i] = y[i]; }
+            for (int k = 0; k < COUNT / 8; ++k) {
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(src + c * 32 + 8 * k);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw->w[c * COUNT / 2 + 4 * k + i] = x[i];
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) raw->w[c][i] = at[2 * i] | (uint32_t)at[2 * i + 1] << 16;
+            for (int i = 0; i < COUNT / 2; ++i) raw->w[c * COUNT / 2 + i] = src[c * 32 + 2 * i] | (uint32_t)src[c * 32 + 2 * i + 1] << 16;
         }
     }
 }
-template <int NC>
-__device__ inline float convert_query(const AttendArgs &a, const QueryRaw<NC> &raw, half8 *q) {
+template <int ROWS, int NW>
+__device__ inline float convert_query(const AttendArgs &a, const QueryRaw<NW> &raw, half8 *q) {
     if (!a.bf16) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const half2v two = __builtin_bit_cast(half2v, raw.w[c][i]);
-                q[2 * c + i / 4][2 * (i % 4)] = two[0];
-                q[2 * c + i / 4][2 * (i % 4) + 1] = two[1];
-            }
+        for (int i = 0; i < NW; ++i) {
+            const half2v two = __builtin_bit_cast(half2v, raw.w[i]);
+            q[i / 4][2 * (i % 4)] = two[0];
+            q[i / 4][2 * (i % 4) + 1] = two[1];
+        }
         return 1.0f;
     }
     float top = 0.0f;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw.w[c][i] << 16)), fabsf(__uint_as_float(raw.w[c][i] & 0xffff0000u))));
-    top = other_half_max(top);
+    for (int i = 0; i < NW; ++i)
+        top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw.w[i] << 16)), fabsf(__uint_as_float(raw.w[i] & 0xffff0000u))));
+    top = row_max<ROWS>(top);
     uint32_t e = __float_as_uint(top) >> 23;
     e = e < 15u ? 15u : e;
     const float scale = __uint_as_float((e - 14u) << 23);              // 2^(exponent - 14): the largest comes to lie in [2^14, 2^15)
     const float inv = __uint_as_float((268u - e) << 23);               // 1 / scale (Inf in a row leaves Inf or NaN in it either way)
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            q[2 * c + i / 4][2 * (i % 4)] = (_Float16)(__uint_as_float(raw.w[c][i] << 16) * inv);
-            q[2 * c + i / 4][2 * (i % 4) + 1] = (_Float16)(__uint_as_float(raw.w[c][i] & 0xffff0000u) * inv);
-        }
+    for (int i = 0; i < NW; ++i) {
+        q[i / 4][2 * (i % 4)] = (_Float16)(__uint_as_float(raw.w[i] << 16) * inv);
+        q[i / 4][2 * (i % 4) + 1] = (_Float16)(__uint_as_float(raw.w[i] & 0xffff0000u) * inv);
+    }
     return scale;
 }
 
@@ -331,25 +361,26 @@ struct Lookup {
 };
 
 // x of a block's tokens from its raw products: visible are those before `limit`.
-__device__ inline void some_of_block(const f32x16 &s, float kc, float lb, uint32_t j, int32_t limit, float *x, float *top, float *tope) {
-    const int32_t left = limit - (int32_t)(j * 32u) - 4 * (int32_t)((uint32_t)lane_id() >> 5);
+template <int ROWS, typename S>
+__device__ inline void some_of_block(const S &s, float kc, float lb, uint32_t j, int32_t limit, float *x, float *top, float *tope) {
+    const int32_t left = limit - (int32_t)(j * 32u) - (int32_t)token_of<ROWS>(0);
     float best = kNegInf;
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
+    for (int t = 0; t < kScores<ROWS>; ++t) {
         const float v = s[t] * kc;
-        x[t] = 8 * (t / 4) + t % 4 < left ? v : kNegInf;
+        x[t] = (ROWS == 32 ? 8 : 16) * (t / 4) + t % 4 < left ? v : kNegInf;
         best = fmaxf(best, x[t]);
     }
-    *top = other_half_max(best);
+    *top = row_max<ROWS>(best);
     *tope = *top + lb;                        // (NaN for a poisoned block: no reference follows it)
 }
 // x and lv (weights_each) of the open block's tokens, with their own scales; `held` of its tokens are there.
-__device__ inline void each_of_open(const f32x16 &s, float qc, const float *ke, uint32_t held, uint32_t j, int32_t limit, float *x, float *lv, float *top, float *tope) {
-    const uint32_t h = (uint32_t)lane_id() >> 5;
+template <int ROWS, typename S>
+__device__ inline void each_of_open(const S &s, float qc, const float *ke, uint32_t held, uint32_t j, int32_t limit, float *x, float *lv, float *top, float *tope) {
     float best = kNegInf, bests = kNegInf;
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
-        const uint32_t tok = 8u * (t / 4) + 4u * h + t % 4;
+    for (int t = 0; t < kScores<ROWS>; ++t) {
+        const uint32_t tok = token_of<ROWS>(t);
         const bool see = tok < held && (int32_t)(j * 32u + tok) < limit;
         const float kt = ke[tok], vt = ke[32u + tok];
         x[t] = see ? s[t] * (kt * qc) : kNegInf;
@@ -357,8 +388,8 @@ __device__ inline void each_of_open(const f32x16 &s, float qc, const float *ke, 
         best = fmaxf(best, x[t]);
         bests = fmaxf(bests, x[t] + lv[t]);
     }
-    *top = other_half_max(best);
-    *tope = other_half_max(bests);
+    *top = row_max<ROWS>(best);
+    *tope = row_max<ROWS>(bests);
 }
 // The open block's values as an operand: places nobody has written yet may hold anything.
 __device__ inline half8 open_values(const uint8_t *at, uint32_t u, uint32_t held) {
@@ -373,6 +404,7 @@ __device__ inline float log_sum(float m, float l) {                     // natur
     return l > 0.0f ? (m + __log2f(l)) * 0.6931471805599453f : (l == l ? kNegInf : l);
 }
 __device__ inline f32x16 mfma(half8 a, half8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mfma(half8 a, half8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ inline void store_out(const AttendArgs &a, const RowPlace &p, uint32_t d, f32x4 v) {
     uint16_t *dst = reinterpret_cast<uint16_t *>(a.out.p) + p.token * a.out.token + (int64_t)p.qh * a.out.head + d;
     uint16_t w[4];

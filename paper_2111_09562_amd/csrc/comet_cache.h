@@ -103,6 +103,8 @@ struct AttendArgs {
 };
 template <int NC>
 __global__ void k_attend(AttendArgs a);
+template <int NC>
+__global__ void k_attend_few(AttendArgs a);
 template <int NC, int RT>
 __global__ void k_attend_tile(AttendArgs a);
 __global__ void k_attend_join(AttendArgs a);
@@ -110,6 +112,7 @@ __global__ void k_attend_join_tile(AttendArgs a);
 
 // ---- types ------------------------------------------------------------------------------------------------------
 using half8 = _Float16 __attribute__((ext_vector_type(8)));
+using half4 = _Float16 __attribute__((ext_vector_type(4)));
 using half2v = _Float16 __attribute__((ext_vector_type(2)));
 using f32x16 = float __attribute__((ext_vector_type(16)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
@@ -232,8 +235,7 @@ struct Seq {
     int32_t start, n, len;      // first token in the batch, new tokens, tokens held once they are in
 };
 // false: the batch's numbers for this sequence make no sense (reported) or it has no tokens in the batch
-__device__ inline bool read_sequence(const BatchArgs &b, uint32_t seq, Seq *s) {
-    const int32_t s0 = b.starts[seq], s1 = b.starts[seq + 1], len = b.lens[seq];
+__device__ inline bool check_sequence(const BatchArgs &b, int32_t s0, int32_t s1, int32_t len, Seq *s) {
     if (s0 < 0 || s1 < s0 || s1 > (int32_t)b.n_tokens || len < 0 || len > kMaxLen) {
         raise(b.status);
         return false;
@@ -241,14 +243,49 @@ __device__ inline bool read_sequence(const BatchArgs &b, uint32_t seq, Seq *s) {
     s->start = s0; s->n = s1 - s0; s->len = len;
     return s->n > 0;
 }
+__device__ inline bool check_slot(const BatchArgs &b, const CacheArgs &c, int32_t v) {
+    if (v >= 0 && (uint32_t)v < c.n_slots) return true;
+    raise(b.status);
+    return false;
+}
 __device__ inline bool read_slot(const BatchArgs &b, const CacheArgs &c, uint32_t seq, uint32_t *slot) {
     const int32_t v = b.slots ? b.slots[seq] : (int32_t)seq;
-    if (v < 0 || (uint32_t)v >= c.n_slots) {
+    *slot = (uint32_t)v;
+    return check_slot(b, c, v);
+}
+// The sequence whose blocks of new tokens `unit` is among (first_unit with shift 5, mul 1, extra 2), its numbers and its slot (unchecked), and
+// which of its blocks that is.  Once 64 sequences are left everything about them is loaded at once: a step of up to 64 sequences
+// waits for one load here instead of three.
+struct Unit {
+    uint32_t seq, block;
+    int32_t slot;
+    Seq s;
+};
+__device__ inline bool find_block(const BatchArgs &b, uint32_t unit, Unit *u) {
+    uint32_t lo = 0, len = b.n_seqs;
+    while (len > 64u) {
+        const uint32_t stride = (len + 63u) / 64u, off = (uint32_t)lane_id() * stride;
+        const bool le = off < len && first_unit(b.starts, lo + off, 1u, 5u, 2u) <= unit;
+        const uint32_t n = (uint32_t)__popcll(wave_ballot(le)), k = n > 0u ? n - 1u : 0u;
+        lo += k * stride;
+        len = len - k * stride < stride ? len - k * stride : stride;
+    }
+    const uint32_t mine = (uint32_t)lane_id() < len ? lo + (uint32_t)lane_id() : lo;
+    const int32_t s0 = b.starts[mine], s1 = b.starts[mine + 1u], held = b.lens[mine], slot = b.slots ? b.slots[mine] : (int32_t)mine;
+    const uint32_t first = ((uint32_t)s0 >> 5) + 2u * mine;
+    const uint32_t n = (uint32_t)__popcll(wave_ballot((uint32_t)lane_id() < len && first <= unit));
+    const int k = (int)(n > 0u ? n - 1u : 0u);
+    const auto of = [k](int32_t v) { return __builtin_amdgcn_readlane(v, k); };
+    u->seq = lo + (uint32_t)k;
+    u->slot = of(slot);
+    const uint32_t f = (uint32_t)of((int32_t)first);
+    if (!check_sequence(b, of(s0), of(s1), of(held), &u->s) || unit < f) return false;
+    if (u->s.len < u->s.n) {
         raise(b.status);
         return false;
     }
-    *slot = (uint32_t)v;
-    return true;
+    u->block = (uint32_t)(u->s.len - u->s.n) / kBlk + (unit - f);
+    return u->block <= (uint32_t)(u->s.len - 1) / kBlk;
 }
 // Index of block j of a sequence's head among all blocks of the cache, or -1 (reported): behind the table's end or no page.
 __device__ inline int64_t block_index(const BatchArgs &b, const CacheArgs &c, uint32_t seq, uint32_t head, uint32_t j) {

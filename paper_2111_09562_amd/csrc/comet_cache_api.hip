@@ -87,10 +87,14 @@ void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tok
     k_rope<T, V><<<wg, kRopeBlock, 0, st>>>(r, g, x, y, n_tokens, heads, dim, sign);
 }
 
-constexpr uint32_t kAttendPieces = 768, kAttendTilePieces = 512;     // workgroups an attention call is cut into, about
+// Workgroups an attention call is cut into, about.  Few rows: 768 are resident at once for heads of 128; many sequences of different lengths
+// (64 x 400 .. 16384 tokens, 8 heads) take 122 us with 768, 127 with 512, two long ones (120000 tokens, 8 heads) 104 with 768, 99 with 512.
+// Many rows: beyond 512 pieces what they leave for the join costs more than shorter pieces save (prompts of 500 to 2000 tokens, 8 heads: 117 us
+// with 512, 153 with 768).
+constexpr uint32_t kAttendPieces = 768, kAttendPiecesLong = 512, kAttendTilePieces = 512;
 struct AttendPlan {
     uint32_t pieces, slots, tiles, tile_shift, min_blocks;
-    bool wide, two;                                      // k_attend_tile; with two tiles of 32 rows per wavefront
+    bool few, wide, two;                                 // k_attend_few; k_attend_tile; that with two tiles of 32 rows per wavefront
     uint64_t off_s, off_dir, bytes;
 };
 bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads, AttendPlan *p) {
@@ -101,9 +105,10 @@ bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32
     // Tiles of 256 rows for heads of up to 64, of 128 for those beyond 128 (what fits the registers); between, 256 rows once prompts are long:
     // 8 x 4 heads of 128, prompts of 500 to 4096 tokens 137 us (128 rows: 123), 4096 tokens behind 28672 2.10 ms (2.26).
     p->two = s.dim <= 64u || (s.dim <= 128u && n_tokens / 4096u >= n_seqs);
-    p->tile_shift = !p->wide ? 5u : p->two ? 8u : 7u;
+    p->few = rows <= 16ull * n_seqs;
+    p->tile_shift = p->few ? 4u : !p->wide ? 5u : p->two ? 8u : 7u;
     p->tiles = (uint32_t)(rows >> p->tile_shift) + n_seqs;
-    p->pieces = ((p->wide ? kAttendTilePieces : kAttendPieces) + s.heads - 1u) / s.heads;
+    p->pieces = ((p->wide ? kAttendTilePieces : (uint64_t)p->tiles * s.heads < 128u ? kAttendPiecesLong : kAttendPieces) + s.heads - 1u) / s.heads;
     p->min_blocks = p->wide ? 16u : 4u;
     // a tile's pieces are counted as if it saw all of its sequence: of tiles of a causal prompt up to half have nothing to do
     p->slots = (p->wide ? 2u : 1u) * p->pieces + p->tiles;
@@ -127,7 +132,8 @@ void launch_attend(const AttendArgs &a, const AttendPlan &p, uint32_t wg, hipStr
             k_attend_tile<NC, 1><<<wg, kAttendBlock, 0, st>>>(a);
             return;
         }
-    k_attend<NC><<<wg, kAttendBlock, 0, st>>>(a);
+    if (p.few) k_attend_few<NC><<<wg, kAttendBlock, 0, st>>>(a);
+    else k_attend<NC><<<wg, kAttendBlock, 0, st>>>(a);
 }
 
 }  // namespace
@@ -277,7 +283,7 @@ int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const com
     if (p.wide) {
         k_attend_join_tile<<<dim3(groups, 8u), kAttendBlock, 0, st>>>(a);
     } else {
-        uint32_t side = 2048u / groups;                  // the rows of a tile side by side while there are few tiles
+        uint32_t side = 4096u / groups;                 // the rows of a tile side by side while there are few tiles
         side = side < 1u ? 1u : (side > a.tile_rows ? a.tile_rows : side);
         k_attend_join<<<dim3(groups, side), kAttendBlock, 0, st>>>(a);
     }

@@ -15,8 +15,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
     const uint32_t number = blockIdx.x / a.c.heads, head = blockIdx.x - number * a.c.heads;
     Piece p;
     if (!find_piece(a, number, &p)) return;
-    Seq s;
-    if (!read_sequence(a.b, p.seq, &s)) return;
+    const Seq s = p.s;
     const RowPlace place = row_place(a, s, head, p.tile * 32u + n);
     int32_t least, most;
     row_limits(a, s, p.tile * 32u, 32u, &least, &most);
@@ -25,9 +24,9 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
     const uint32_t j0 = (uint32_t)((uint64_t)seen * p.part / parts), j1 = (uint32_t)((uint64_t)seen * (p.part + 1u) / parts);
     const uint32_t whole = (uint32_t)s.len / 32u;                                             // complete blocks
 
-    QueryRaw<NC> raw;
-    request_query<NC>(a, place, &raw);
-    RowState<NC> row;
+    QueryRaw<8 * NC> raw;
+    request_query<NC, 16>(a, place, 16u * h, &raw);
+    RowState<NC, f32x16, 32> row;
     row.clear();
 
     // the wavefront's blocks: j0 + wave, j0 + wave + 4, ...; where they lie is looked up for 64 of them at a time
@@ -37,7 +36,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
     Lookup look;
     look.get(a, p.seq, head, j + 4u * lane, end);
     half8 q[2 * NC];
-    const float qc = convert_query<NC>(a, raw, q) * a.scale;
+    const float qc = convert_query<32>(a, raw, q) * a.scale;
     while (j < end) {
         const uint32_t left = (end - j + 3u) / 4u, count = left < 64u ? left : 64u;
         const auto load = [&](u32x4 *to, int64_t at, uint32_t which) {
@@ -67,18 +66,18 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
                 float best = acc[0];
 #pragma unroll
                 for (int t = 1; t < 16; ++t) best = fmaxf(best, acc[t]);
-                top = other_half_max(best) * kc;
+                top = row_max<32>(best) * kc;
                 tope = top + lb;
             } else {
                 float x[16];
-                some_of_block(acc, kc, lb, j, limit, x, &top, &tope);
+                some_of_block<32>(acc, kc, lb, j, limit, x, &top, &tope);
             }
             row.follow(top, tope);
             if (all) {
                 row.weights(acc, kc, lb, pw);
             } else {
                 float x[16];
-                some_of_block(acc, kc, lb, j, limit, x, &top, &tope);
+                some_of_block<32>(acc, kc, lb, j, limit, x, &top, &tope);
                 row.weights_some(x, lb, pw);
             }
 #pragma unroll
@@ -105,7 +104,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
                 for (int u = 0; u < 2; ++u)
                     acc = mfma(*reinterpret_cast<const half8 *>(half + 2048u * c + 64u * n + 32u * h + 16u * u), q[2 * c + u], acc);
             float x[16], lv[16], top, tope;
-            each_of_open(acc, qc, reinterpret_cast<const float *>(half + 128ull * dim), held, j, place.limit, x, lv, &top, &tope);
+            each_of_open<32>(acc, qc, reinterpret_cast<const float *>(half + 128ull * dim), held, j, place.limit, x, lv, &top, &tope);
             row.follow(top, tope);
             half8 pw[2];
             row.weights_each(x, lv, pw);
@@ -118,7 +117,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
     }
 
     // The four wavefronts' results in one, in their order.
-    row.l += other_half(row.l);
+    row.l = row_sum<32>(row.l);
     if (h == 0u) { s_stat[wave][0][n] = row.m; s_stat[wave][1][n] = row.l; s_stat[wave][2][n] = row.r; }
     __syncthreads();
     float mm = kNegInf, rr = kNegInf, ll = 0.0f;
@@ -161,6 +160,180 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
         const uint32_t d = 32u * c + 8u * wave + 4u * h;
         if (place.real && last) store_out(a, place, d, sum);
         else if (place.real) *reinterpret_cast<f32x4 *>(a.part_o + (slot_no + n) * dim + d) = sum;
+    }
+}
+
+// Fewer still: the same with tiles of 16 rows, half the registers and so twice the wavefronts and loads in flight.  Bound by HBM.
+template <int NC>
+__global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k_attend_few(AttendArgs a) {
+    constexpr uint32_t dim = 32u * NC;
+    __shared__ float s_stat[4][3][16];
+    __shared__ __align__(16) float s_tile[4][1024];
+    const uint32_t lane = (uint32_t)lane_id(), wave = threadIdx.x / kWave, n = lane & 15u, g = lane >> 4;
+    const uint32_t number = blockIdx.x / a.c.heads, head = blockIdx.x - number * a.c.heads;
+    Piece p;
+    if (!find_piece(a, number, &p)) return;
+    const Seq s = p.s;
+    const RowPlace place = row_place(a, s, head, p.tile * 16u + n);
+    int32_t least, most;
+    row_limits(a, s, p.tile * 16u, 16u, &least, &most);
+    const uint32_t seen = most > 0 ? ((uint32_t)most + 31u) / 32u : 0u, parts = parts_of(seen, p.per);
+    if (p.part >= parts) return;
+    const uint32_t j0 = (uint32_t)((uint64_t)seen * p.part / parts), j1 = (uint32_t)((uint64_t)seen * (p.part + 1u) / parts);
+    const uint32_t whole = (uint32_t)s.len / 32u;                                             // complete blocks
+
+    // of 32 values of the head a lane's operands have the eight from `chunk` on
+    const uint32_t chunk = 16u * (g & 1u) + 8u * (g >> 1);
+    QueryRaw<4 * NC> raw;
+    request_query<NC, 8>(a, place, chunk, &raw);
+    RowState<2 * NC, f32x4, 16> row;
+    row.clear();
+
+    // the wavefront's blocks: j0 + wave, j0 + wave + 4, ...; where they lie is looked up for 64 of them at a time
+    uint32_t j = j0 + wave;
+    const uint32_t end = j1 < whole ? j1 : whole;
+    u32x4 kr[NC], vr[NC];
+    Lookup look;
+    look.get(a, p.seq, head, j + 4u * lane, end);
+    half8 q[NC];
+    const float qc = convert_query<16>(a, raw, q) * a.scale;
+    while (j < end) {
+        const uint32_t left = (end - j + 3u) / 4u, count = left < 64u ? left : 64u;
+        const auto load = [&](u32x4 *to, int64_t at, uint32_t which) {
+            const uint8_t *from = a.c.blocks + (uint64_t)(at < 0 ? 0 : at) * (64u * dim) + which * (32u * dim) + n * 32u + (g >> 1) * 512u + (g & 1u) * 16u;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) to[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024);
+        };
+        int64_t at = look.index_of(0);
+        load(kr, at, 0u);
+        load(vr, at, 1u);
+        for (uint32_t i = 0; i < count; ++i, j += 4u) {
+            const int64_t next = i + 1u < count ? look.index_of(i + 1u) : -1;
+            // Lane l has loaded 16 values of one token (l & 15, 16 more in the upper half of the wavefront), the instruction wants eight of the token
+            // l & 15 of either half: one exchange between the halves per two registers.
+            f32x4 acc[2] = {};
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const auto x = __builtin_amdgcn_permlane32_swap(kr[c][0], kr[c][2], false, false), y = __builtin_amdgcn_permlane32_swap(kr[c][1], kr[c][3], false, false);
+                acc[0] = mfma(whole8(x[0], y[0]), q[c], acc[0]);
+                acc[1] = mfma(whole8(x[1], y[1]), q[c], acc[1]);
+            }
+            const float sc[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3], acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
+            if (next >= 0) load(kr, next, 0u);
+            const float kc = Lookup::of(look.ks, i) * qc, lb = Lookup::of(look.lb, i);
+            half8 pw[1];
+            // (one place that moves the references, and x once more behind it: two such places cost a hundred registers)
+            const bool all = at >= 0 && (int32_t)(j * 32u + 32u) <= least && lb == lb;
+            const int32_t limit = at >= 0 ? place.limit : 0;
+            float top, tope;
+            if (all) {
+                float best = sc[0];
+#pragma unroll
+                for (int t = 1; t < 8; ++t) best = fmaxf(best, sc[t]);
+                top = row_max<16>(best) * kc;
+                tope = top + lb;
+            } else {
+                float x[8];
+                some_of_block<16>(sc, kc, lb, j, limit, x, &top, &tope);
+            }
+            row.follow(top, tope);
+            if (all) {
+                row.weights(sc, kc, lb, pw);
+            } else {
+                float x[8];
+                some_of_block<16>(sc, kc, lb, j, limit, x, &top, &tope);
+                row.weights_some(x, lb, pw);
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const auto x = __builtin_amdgcn_permlane32_swap(vr[c][0], vr[c][1], false, false), y = __builtin_amdgcn_permlane32_swap(vr[c][2], vr[c][3], false, false);
+                row.o[2 * c] = mfma(whole8(x[0], y[0]), pw[0], row.o[2 * c]);
+                row.o[2 * c + 1] = mfma(whole8(x[1], y[1]), pw[0], row.o[2 * c + 1]);
+            }
+            if (next >= 0) load(vr, next, 1u);
+            at = next;
+        }
+        if (j < end) look.get(a, p.seq, head, j + 4u * lane, end);
+    }
+
+    // the open block, in 16 bits, with a scale for every token
+    if (j == whole && j < j1) {
+        uint32_t slot;
+        if (read_slot(a.b, a.c, p.seq, &slot)) {
+            const uint8_t *half = ring_half(a.c, slot, head, j);
+            const uint32_t held = (uint32_t)s.len % 32u;
+            f32x4 acc[2] = {};
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (uint32_t t = 0; t < 2u; ++t)
+                    acc[t] = mfma(*reinterpret_cast<const half8 *>(half + 2048u * c + 64u * (16u * t + n) + 2u * chunk), q[c], acc[t]);
+            const float sc[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3], acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
+            float x[8], lv[8], top, tope;
+            each_of_open<16>(sc, qc, reinterpret_cast<const float *>(half + 128ull * dim), held, j, place.limit, x, lv, &top, &tope);
+            row.follow(top, tope);
+            half8 pw[1];
+            row.weights_each(x, lv, pw);
+#pragma unroll
+            for (int c = 0; c < 2 * NC; ++c) {
+                const uint8_t *from = half + 64u * dim + 64u * (16u * c + n) + 32u * (g & 1u) + 8u * (g >> 1);
+                half8 v;
+#pragma unroll
+                for (uint32_t u = 0; u < 2u; ++u) {
+                    const half4 part = *reinterpret_cast<const half4 *>(from + 16u * u);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)                             // places nobody has written yet may hold anything
+                        v[4 * u + i] = 16u * u + 4u * g + i < held ? part[i] : (_Float16)0.0f;
+                }
+                row.o[c] = mfma(v, pw[0], row.o[c]);
+            }
+        }
+    }
+
+    // The four wavefronts' results in one, in their order.
+    row.l = row_sum<16>(row.l);
+    if (g == 0u) { s_stat[wave][0][n] = row.m; s_stat[wave][1][n] = row.l; s_stat[wave][2][n] = row.r; }
+    __syncthreads();
+    float mm = kNegInf, rr = kNegInf, ll = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) { mm = fmaxf(mm, s_stat[w][0][n]); rr = fmaxf(rr, s_stat[w][2][n]); }
+    const float mms = mm == kNegInf ? 0.0f : mm, rrs = rr == kNegInf ? 0.0f : rr;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) ll += s_stat[w][1][n] * exp2_fast(s_stat[w][0][n] - mms);
+    const float mine = exp2_fast(row.r - rrs);
+    const bool last = parts == 1u;
+    const uint64_t slot_no = ((uint64_t)p.number * a.c.heads + head) * 16u;
+    if (wave == 0u && g == 0u) {
+        if (last) {
+            if (place.real && a.lse) a.lse[place.token * a.q_heads + place.qh] = log_sum(mms, ll);
+        } else {
+            float *st = a.part_s + 3u * (slot_no + n);
+            st[0] = mm; st[1] = ll; st[2] = rr;
+        }
+        if (p.part == 0u && head == 0u && n == 0u) {
+            int32_t *dir = a.directory + 2u * (first_unit(a.b.starts, p.seq, a.group, a.tile_shift, 1u) + p.tile);
+            dir[0] = (int32_t)p.number;
+            dir[1] = (int32_t)parts;
+        }
+    }
+    // o of a row without tokens is 0
+    const float fin = last ? (ll == 0.0f ? 0.0f : exp2_fast(rrs - mms - kLift) / ll) : 1.0f;
+#pragma unroll
+    for (int c = 0; c < 2 * NC; c += 4) {                                   // 64 values of the head at a time, 16 of them per wavefront
+        if (c) __syncthreads();
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            if (c + t < 2 * NC) *reinterpret_cast<f32x4 *>(&s_tile[wave][256 * t + 4 * lane]) = row.o[c + t] * mine;
+        __syncthreads();
+        if (c + (int)wave < 2 * NC) {
+            f32x4 sum = *reinterpret_cast<const f32x4 *>(&s_tile[0][256 * wave + 4 * lane]);
+#pragma unroll
+            for (int w = 1; w < 4; ++w) sum += *reinterpret_cast<const f32x4 *>(&s_tile[w][256 * wave + 4 * lane]);
+            sum *= fin;
+            const uint32_t d = 16u * (c + wave) + 4u * g;
+            if (place.real && last) store_out(a, place, d, sum);
+            else if (place.real) *reinterpret_cast<f32x4 *>(a.part_o + (slot_no + n) * dim + d) = sum;
+        }
     }
 }
 
@@ -259,5 +432,13 @@ template __global__ void k_attend<5>(AttendArgs);
 template __global__ void k_attend<6>(AttendArgs);
 template __global__ void k_attend<7>(AttendArgs);
 template __global__ void k_attend<8>(AttendArgs);
+template __global__ void k_attend_few<1>(AttendArgs);
+template __global__ void k_attend_few<2>(AttendArgs);
+template __global__ void k_attend_few<3>(AttendArgs);
+template __global__ void k_attend_few<4>(AttendArgs);
+template __global__ void k_attend_few<5>(AttendArgs);
+template __global__ void k_attend_few<6>(AttendArgs);
+template __global__ void k_attend_few<7>(AttendArgs);
+template __global__ void k_attend_few<8>(AttendArgs);
 
 }  // namespace comet

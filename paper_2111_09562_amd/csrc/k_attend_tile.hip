@@ -33,8 +33,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
     const uint32_t number = blockIdx.x / a.c.heads, head = blockIdx.x - number * a.c.heads;
     Piece p;
     if (!find_piece(a, number, &p)) return;
-    Seq s;
-    if (!read_sequence(a.b, p.seq, &s)) return;
+    const Seq s = p.s;
     int32_t least, most;
     row_limits(a, s, p.tile * rows_wg, rows_wg, &least, &most);
     const uint32_t seen = most > 0 ? ((uint32_t)most + 31u) / 32u : 0u, parts = parts_of(seen, p.per);
@@ -45,12 +44,12 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
     RowPlace place[RT];
     half8 q[RT][2 * NC];
     float qc[RT];
-    QueryRaw<NC> raw[RT];
-    RowState<NC> row[RT];
+    QueryRaw<8 * NC> raw[RT];
+    RowState<NC, f32x16, 32> row[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         place[rt] = row_place(a, s, head, row0 + 32u * rt + n);
-        request_query<NC>(a, place[rt], &raw[rt]);
+        request_query<NC, 16>(a, place[rt], 16u * h, &raw[rt]);
         row[rt].clear();
     }
 
@@ -91,7 +90,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
         float best = acc[0];
 #pragma unroll
         for (int t = 1; t < 16; ++t) best = fmaxf(best, acc[t]);
-        return other_half_max(best);
+        return row_max<32>(best);
     };
 
     uint32_t j = j0;
@@ -107,7 +106,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
     Lookup look;
     look.get(a, p.seq, head, j + lane, end);
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) qc[rt] = convert_query<NC>(a, raw[rt], q[rt]) * a.scale;
+    for (int rt = 0; rt < RT; ++rt) qc[rt] = convert_query<32>(a, raw[rt], q[rt]) * a.scale;
 
     while (j < end) {
         const uint32_t count = end - j < 64u ? end - j : 64u;
@@ -197,7 +196,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
                 for (int rt = 0; rt < RT; ++rt) {
                     const f32x16 acc = products(op, rt);
                     float x[16], top, tope;
-                    some_of_block(acc, ks * qc[rt], lb, jj, place[rt].limit, x, &top, &tope);
+                    some_of_block<32>(acc, ks * qc[rt], lb, jj, place[rt].limit, x, &top, &tope);
                     row[rt].follow(top, tope);
                     row[rt].weights_some(x, lb, pw[rt]);
                 }
@@ -234,7 +233,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
             for (int rt = 0; rt < RT; ++rt) {
                 const f32x16 acc = products(op, rt);
                 float x[16], lv[16], top, tope;
-                each_of_open(acc, qc[rt], reinterpret_cast<const float *>(half + 128ull * dim), held, whole, place[rt].limit, x, lv, &top, &tope);
+                each_of_open<32>(acc, qc[rt], reinterpret_cast<const float *>(half + 128ull * dim), held, whole, place[rt].limit, x, lv, &top, &tope);
                 row[rt].follow(top, tope);
                 row[rt].weights_each(x, lv, pw[rt]);
             }
@@ -251,8 +250,8 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        RowState<NC> &r = row[rt];
-        const float l = r.l + other_half(r.l);
+        const auto &r = row[rt];
+        const float l = row_sum<32>(r.l);
         const float ms = r.m == kNegInf ? 0.0f : r.m, rs = r.r == kNegInf ? 0.0f : r.r;
         if (parts == 1u) {
             const float fin = l == 0.0f ? 0.0f : exp2_fast(rs - ms - kLift) / l;

@@ -12,26 +12,26 @@ template <typename T> __device__ inline uint16_t narrow(float v) { return __buil
 template <typename T> constexpr uint32_t kInf16 = 0x7f80u;              // |bits| from here on: Inf and NaN
 template <> constexpr uint32_t kInf16<_Float16> = 0x7c00u;
 
-// The new rows of a block and those the ring holds of it, in LDS: [32][dim + 8], the keys rotated and rounded to T.  The
+// The rows r0 .. of a block that are new and, with `old`, those the ring holds of it, in LDS: [32][dim + 8], the keys rotated and rounded to T.  The
 // cache compresses the 16-bit keys that a model working in T would keep, so it does not matter in how many calls a
 // block's tokens came.
 template <typename T, int V>
-__device__ void load_block(const AppendArgs &a, const Seq &s, uint32_t before, uint32_t head, uint32_t slot, uint32_t j, uint16_t *kt, uint16_t *vt) {
-    const uint32_t dim = a.c.dim, pitch = dim + 8u, len = (uint32_t)s.len;
+__device__ void load_block(const AppendArgs &a, const Seq &s, uint32_t before, uint32_t head, uint32_t slot, uint32_t j, uint32_t r0, uint32_t r1, bool old,
+                           uint16_t *kt, uint16_t *vt) {
+    const uint32_t dim = a.c.dim, pitch = dim + 8u;
     const uint32_t rot = a.rope.steps ? a.rope.rot : 0u;
     const uint32_t rot_chunks = rot / (2u * V), chunks = rot_chunks + (dim - rot) / V;
-    for (uint32_t i = threadIdx.x; i < kBlk * chunks; i += kCacheBlock) {
-        const uint32_t row = i / chunks, c = i - row * chunks, t = j * kBlk + row;
-        if (t < before || t >= len) continue;
+    for (uint32_t i = threadIdx.x; i < (r1 - r0) * chunks; i += kCacheBlock) {
+        const uint32_t row = r0 + i / chunks, c = i % chunks, t = j * kBlk + row;
         const int32_t token = s.start + (int32_t)(t - before);
         const T *p = reinterpret_cast<const T *>(a.k.p) + (int64_t)token * a.k.token + (int64_t)head * a.k.head;
         float x[V], y[V];
         if (c < rot_chunks) {
             float sn[V], cs[V];
-            chunk_angles<V>(a.rope, c, a.rope.positions ? a.rope.positions[token] : (int32_t)t, 0u, sn, cs);
             const uint32_t at = chunk_at<V>(a.rope, c), second = at + chunk_second<V>(a.rope);
             load_row<T, V>(x, p + at);
             load_row<T, V>(y, p + second);
+            chunk_angles<V>(a.rope, c, a.rope.positions ? a.rope.positions[token] : (int32_t)t, 0u, sn, cs);
             chunk_turn<V>(a.rope.interleaved, x, y, sn, cs);
             store_row<T, V>(reinterpret_cast<T *>(kt + row * pitch + at), x);
             store_row<T, V>(reinterpret_cast<T *>(kt + row * pitch + second), y);
@@ -41,27 +41,30 @@ __device__ void load_block(const AppendArgs &a, const Seq &s, uint32_t before, u
             store_row<T, V>(reinterpret_cast<T *>(kt + row * pitch + at), x);
         }
     }
-    for (uint32_t i = threadIdx.x; i < kBlk * (dim / V); i += kCacheBlock) {
-        const uint32_t row = i / (dim / V), d = (i - row * (dim / V)) * V, t = j * kBlk + row;
-        if (t >= before && t < len) {
-            const int32_t token = s.start + (int32_t)(t - before);
-            float x[V];
-            load_row<T, V>(x, reinterpret_cast<const T *>(a.v.p) + (int64_t)token * a.v.token + (int64_t)head * a.v.head + d);
-            store_row<T, V>(reinterpret_cast<T *>(vt + row * pitch + d), x);
-        } else if (t < before) {
-            const uint8_t *half = ring_half(a.c, slot, head, j);
-            const uint16_t *kr = reinterpret_cast<const uint16_t *>(half), *vr = kr + 32u * dim;
-            const float *e = reinterpret_cast<const float *>(half + 128ull * dim);
+    for (uint32_t i = threadIdx.x; i < (r1 - r0) * (dim / V); i += kCacheBlock) {
+        const uint32_t row = r0 + i / (dim / V), d = i % (dim / V) * V, t = j * kBlk + row;
+        const int32_t token = s.start + (int32_t)(t - before);
+        float x[V];
+        load_row<T, V>(x, reinterpret_cast<const T *>(a.v.p) + (int64_t)token * a.v.token + (int64_t)head * a.v.head + d);
+        store_row<T, V>(reinterpret_cast<T *>(vt + row * pitch + d), x);
+    }
+    if (!old) return;
+    const uint8_t *half = ring_half(a.c, slot, head, j);
+    const uint16_t *kr = reinterpret_cast<const uint16_t *>(half), *vr = kr + 32u * dim;
+    const float *e = reinterpret_cast<const float *>(half + 128ull * dim);
+    for (uint32_t i = threadIdx.x; i < r0 * (dim / 8u); i += kCacheBlock) {        // (r0 <= 31 tokens of before)
+        const uint32_t row = i / (dim / 8u), d = i % (dim / 8u) * 8u;
+        const half8 k = *reinterpret_cast<const half8 *>(kr + (d / 32u * 32u + row) * 32u + d % 32u);
 #pragma unroll
-            for (int u = 0; u < V; ++u) {
-                const uint32_t dd = d + u;
-                kt[row * pitch + dd] = narrow<T>(widen<_Float16>(kr[(dd / 32u * 32u + row) * 32u + dd % 32u]) * e[row]);
-                vt[row * pitch + dd] = narrow<T>(widen<_Float16>(vr[dd * 32u + place_of(row)]) * e[32u + row]);
-            }
-        } else {
+        for (uint32_t u = 0; u < 8u; ++u) kt[row * pitch + d + u] = narrow<T>((float)k[u] * e[row]);
+    }
+    for (uint32_t i = threadIdx.x; i < 8u * dim; i += kCacheBlock) {               // four tokens of a value
+        const uint32_t d = i / 8u, row = token_at(4u * (i % 8u));
+        if (row >= r0) continue;
+        const half4 v = *reinterpret_cast<const half4 *>(vr + 4u * i);
 #pragma unroll
-            for (int u = 0; u < V; ++u) kt[row * pitch + d + u] = vt[row * pitch + d + u] = 0;
-        }
+        for (uint32_t u = 0; u < 4u; ++u)
+            if (row + u < r0) vt[(row + u) * pitch + d] = narrow<T>((float)v[u] * e[32u + row + u]);
     }
 }
 
@@ -73,6 +76,130 @@ __device__ inline float token_scale(float amax) {
     return __uint_as_float((e - 14u) << 23);
 }
 
+__device__ inline uint32_t larger16(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// A block's scale from the bits of its largest |value|, and a value in it.  A block with Inf or NaN has the scale NaN.
+struct BlockScale {
+    float scale, inv;
+    __device__ uint32_t to8(float x) const {
+        const float y = __builtin_rintf(x * inv);
+        return inv == 0.0f ? 0u : (uint32_t)(int32_t)__builtin_amdgcn_fmed3f(y, -127.0f, 127.0f) & 0xffu;
+    }
+};
+template <typename T>
+__device__ inline BlockScale block_scale(uint32_t bits) {
+    const float q = widen<T>((uint16_t)bits) / 127.0f;
+    BlockScale s;
+    s.scale = bits >= kInf16<T> ? __uint_as_float(0x7fc00000u) : (q > kMinScale ? q : kMinScale);
+    s.inv = bits >= kInf16<T> ? 0.0f : 1.0f / s.scale;
+    return s;
+}
+
+// A block all of whose tokens are new, from the tensors to the cache in registers.  A thread has 16 keys of one token (a chunk of eight pairs, or 16
+// values that are not turned) and eight values of four tokens in a row, whose four bytes of a value lie side by side
+// in the cache: a token's eight threads write 32 bytes each of up to 8 kilobytes, eight threads the 32 bytes of a value.
+template <typename T>
+__device__ void compress_block(const AppendArgs &a, const Seq &s, uint32_t before, uint32_t seq, uint32_t head, uint32_t j) {
+    __shared__ uint32_t s_top[2][kCacheBlock / kWave];
+    constexpr int kMost = kCacheMaxDim / 128;              // items of a thread, at most
+    const uint32_t tid = threadIdx.x, dim = a.c.dim, per_row = dim / 16u;
+    const uint32_t rot = a.rope.steps ? a.rope.rot : 0u, rot_chunks = rot / 16u;
+    const int64_t index = block_index(a.b, a.c, seq, head, j);
+    if (index < 0) return;
+    const int32_t token0 = s.start + (int32_t)(j * kBlk - before);
+    typename Vec<T, 8>::type ka[kMost], kb[kMost], v[kMost / 2][4];
+    uint32_t mk = 0, mv = 0;
+    const auto top_of = [](const typename Vec<T, 8>::type &x, uint32_t m) {
+        const u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = larger16(m, larger16(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+        return m;
+    };
+    const auto first_of = [&](uint32_t c) { return c < rot_chunks ? chunk_at<8>(a.rope, c) : rot + 16u * (c - rot_chunks); };
+    const auto second_of = [&](uint32_t c) { return c < rot_chunks ? chunk_second<8>(a.rope) : 8u; };
+#pragma unroll
+    for (int n = 0; n < kMost; ++n) {
+        const uint32_t i = tid + n * kCacheBlock, row = i / per_row, c = i - row * per_row;
+        if (row < (uint32_t)kBlk) {
+            const T *p = reinterpret_cast<const T *>(a.k.p) + (int64_t)(token0 + (int32_t)row) * a.k.token + (int64_t)head * a.k.head + first_of(c);
+            ka[n] = *reinterpret_cast<const typename Vec<T, 8>::type *>(p);
+            kb[n] = *reinterpret_cast<const typename Vec<T, 8>::type *>(p + second_of(c));
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < kMost / 2; ++n) {
+        const uint32_t i = tid + n * kCacheBlock, quad = i % 8u, d = 8u * (i / 8u);
+        if (d < dim) {
+            const T *p = reinterpret_cast<const T *>(a.v.p) + (int64_t)(token0 + 4 * (int32_t)quad) * a.v.token + (int64_t)head * a.v.head + d;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[n][u] = *reinterpret_cast<const typename Vec<T, 8>::type *>(p + u * a.v.token);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < kMost; ++n) {
+        const uint32_t i = tid + n * kCacheBlock, row = i / per_row, c = i - row * per_row;
+        if (row < (uint32_t)kBlk) {
+            if (c < rot_chunks) {
+                float x[8], y[8], sn[8], cs[8];
+                chunk_angles<8>(a.rope, c, a.rope.positions ? a.rope.positions[token0 + (int32_t)row] : (int32_t)(j * kBlk + row), 0u, sn, cs);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) { x[u] = (float)ka[n][u]; y[u] = (float)kb[n][u]; }
+                chunk_turn<8>(a.rope.interleaved, x, y, sn, cs);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) { ka[n][u] = (T)x[u]; kb[n][u] = (T)y[u]; }
+            }
+            mk = top_of(kb[n], top_of(ka[n], mk));
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < kMost / 2; ++n)
+        if (8u * ((tid + n * kCacheBlock) / 8u) < dim) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) mv = top_of(v[n][u], mv);
+        }
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        mk = larger16(mk, (uint32_t)__shfl_xor((int)mk, o, kWave));
+        mv = larger16(mv, (uint32_t)__shfl_xor((int)mv, o, kWave));
+    }
+    if (lane_id() == 0) { s_top[0][tid / kWave] = mk; s_top[1][tid / kWave] = mv; }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t w = 0; w < kCacheBlock / kWave; ++w) { mk = larger16(mk, s_top[0][w]); mv = larger16(mv, s_top[1][w]); }
+    const BlockScale sk = block_scale<T>(mk), sv = block_scale<T>(mv);
+    uint8_t *to = a.c.blocks + (uint64_t)index * 64u * dim;
+#pragma unroll
+    for (int n = 0; n < kMost; ++n) {
+        const uint32_t i = tid + n * kCacheBlock, row = i / per_row, c = i - row * per_row;
+        if (row < (uint32_t)kBlk) {
+            const uint32_t d = first_of(c), e = d + second_of(c);
+            uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                w[u / 4] |= sk.to8((float)ka[n][u]) << (8 * (u % 4));
+                w[2 + u / 4] |= sk.to8((float)kb[n][u]) << (8 * (u % 4));
+            }
+            *reinterpret_cast<uint2 *>(to + d / 32u * 1024u + row * 32u + d % 32u) = uint2{w[0], w[1]};
+            *reinterpret_cast<uint2 *>(to + e / 32u * 1024u + row * 32u + e % 32u) = uint2{w[2], w[3]};
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < kMost / 2; ++n) {
+        const uint32_t i = tid + n * kCacheBlock, quad = i % 8u, d = 8u * (i / 8u);
+        if (d < dim) {
+            uint8_t *at = to + 32u * dim + 32u * d + place_of(4u * quad);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                uint32_t w = 0u;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) w |= sv.to8((float)v[n][u][k]) << (8 * u);
+                *reinterpret_cast<uint32_t *>(at + 32u * k) = w;
+            }
+        }
+    }
+    if (tid < 2u) a.c.scales[2u * (uint64_t)index + tid] = tid ? sv.scale : sk.scale;
+}
+
 }  // namespace
 
 template <typename T>
@@ -80,17 +207,11 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
     extern __shared__ __align__(16) uint16_t s_rows[];
     __shared__ uint32_t s_amax[2][kBlk];
     const uint32_t tid = threadIdx.x, unit = blockIdx.x, dim = a.c.dim, pitch = dim + 8u;
-    const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, 1u, 5u, 2u);
-    Seq s;
-    if (!read_sequence(a.b, seq, &s)) return;
-    const uint32_t first = first_unit(a.b.starts, seq, 1u, 5u, 2u);
-    if (unit < first) return;
-    if (s.len < s.n) {
-        raise(a.b.status);
-        return;
-    }
-    const uint32_t len = (uint32_t)s.len, before = len - (uint32_t)s.n, j0 = before / kBlk, j = j0 + (unit - first);
-    if (j > (len - 1u) / kBlk) return;
+    Unit found;
+    if (!find_block(a.b, unit, &found)) return;
+    const uint32_t seq = found.seq, j = found.block;
+    const Seq s = found.s;
+    const uint32_t len = (uint32_t)s.len, before = len - (uint32_t)s.n, j0 = before / kBlk;
 
     if (blockIdx.y >= a.c.heads) {                         // queries: the block's new tokens, some heads
         const uint32_t h0 = (blockIdx.y - a.c.heads) * a.q_heads_wg;
@@ -135,10 +256,13 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
     }
 
     const uint32_t head = blockIdx.y;
-    uint32_t slot;
-    if (!read_slot(a.b, a.c, seq, &slot)) return;
+    if (!check_slot(a.b, a.c, found.slot)) return;
+    const uint32_t slot = (uint32_t)found.slot, open = len / kBlk;
+    if (a.vec && j * kBlk >= before && j + 1u < open) {     // all of it is new, and the ring does not hold it: no detour
+        compress_block<T>(a, s, before, seq, head, j);
+        return;
+    }
     uint16_t *kt = s_rows, *vt = s_rows + kBlk * pitch;
-    const uint32_t open = len / kBlk;
     // The ring keeps the open block and the one before it, so the length may be set back by up to a block.  A half that holds the
     // beginning of block j0 is overwritten by a later block of the same parity: that one is left to the workgroup
     // of j0, which reads the half first.
@@ -150,27 +274,30 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
     for (uint32_t turn_no = 0; turn_no < (again ? 2u : 1u); ++turn_no) {
         const uint32_t jj = turn_no ? again : j;
         if (turn_no) __syncthreads();
-        if (a.vec) load_block<T, 8>(a, s, before, head, slot, jj, kt, vt);
-        else load_block<T, 1>(a, s, before, head, slot, jj, kt, vt);
+        const uint32_t r0 = jj * kBlk < before ? before - jj * kBlk : 0u;                                      // the block's new rows
+        const uint32_t r1 = len - jj * kBlk < (uint32_t)kBlk ? len - jj * kBlk : (uint32_t)kBlk;
+        const bool whole = !turn_no && j < open;           // complete: the rows the ring holds are needed, too
+        if (a.vec) load_block<T, 8>(a, s, before, head, slot, jj, r0, r1, whole, kt, vt);
+        else load_block<T, 1>(a, s, before, head, slot, jj, r0, r1, whole, kt, vt);
         __syncthreads();
-        {                                                  // largest |value| of every token, as bits: Inf and NaN are the largest
-            const uint32_t row = tid / 8u, part = tid % 8u, per = dim / 8u;
+        const uint32_t mine_row = tid / 8u;
+        if (mine_row < r1 && (whole || mine_row >= r0)) {  // largest |value| of every token, as bits: Inf and NaN are the largest
+            const uint32_t part = tid % 8u;
             uint32_t mk = 0, mv = 0;
-            for (uint32_t d = part * per; d < (part + 1u) * per; ++d) {
-                const uint32_t bk = kt[row * pitch + d] & 0x7fffu, bv = vt[row * pitch + d] & 0x7fffu;
-                mk = bk > mk ? bk : mk;
-                mv = bv > mv ? bv : mv;
+            for (uint32_t d = 2u * part; d < dim; d += 16u) {
+                const uint32_t bk = *reinterpret_cast<const uint32_t *>(kt + mine_row * pitch + d), bv = *reinterpret_cast<const uint32_t *>(vt + mine_row * pitch + d);
+                mk = larger16(mk, larger16(bk & 0x7fffu, bk >> 16 & 0x7fffu));
+                mv = larger16(mv, larger16(bv & 0x7fffu, bv >> 16 & 0x7fffu));
             }
 #pragma unroll
             for (int o = 1; o < 8; o <<= 1) {
-                const uint32_t ok = __shfl_xor(mk, o, kWave), ov = __shfl_xor(mv, o, kWave);
-                mk = ok > mk ? ok : mk;
-                mv = ov > mv ? ov : mv;
+                mk = larger16(mk, (uint32_t)__shfl_xor((int)mk, o, kWave));
+                mv = larger16(mv, (uint32_t)__shfl_xor((int)mv, o, kWave));
             }
-            if (part == 0u) { s_amax[0][row] = mk; s_amax[1][row] = mv; }
+            if (part == 0u) { s_amax[0][mine_row] = mk; s_amax[1][mine_row] = mv; }
         }
         __syncthreads();
-        if (!turn_no && j < open) {                        // complete: compress
+        if (whole) {                                       // compress
             const int64_t index = block_index(a.b, a.c, seq, head, j);
             if (index >= 0) {
                 uint32_t m[2] = {0u, 0u};
@@ -184,17 +311,7 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
                     }
                     m[kind] = v;
                 }
-                float scale[2], inv[2];
-#pragma unroll
-                for (int kind = 0; kind < 2; ++kind) {
-                    const float q = widen<T>((uint16_t)m[kind]) / 127.0f;
-                    scale[kind] = m[kind] >= kInf16<T> ? __uint_as_float(0x7fc00000u) : (q > kMinScale ? q : kMinScale);
-                    inv[kind] = m[kind] >= kInf16<T> ? 0.0f : 1.0f / scale[kind];
-                }
-                const auto to8 = [](float x, float f) -> uint32_t {
-                    const float y = __builtin_rintf(x * f);
-                    return f == 0.0f ? 0u : (uint32_t)(int32_t)(y > 127.0f ? 127.0f : (y < -127.0f ? -127.0f : y)) & 0xffu;
-                };
+                const BlockScale scale[2] = {block_scale<T>(m[0]), block_scale<T>(m[1])};
                 uint8_t *to = a.c.blocks + (uint64_t)index * 64u * dim;
                 for (uint32_t i = tid; i < 4u * dim; i += kCacheBlock) {       // 16 bytes each: keys, then values
                     uint32_t w[4] = {0u, 0u, 0u, 0u};
@@ -202,23 +319,21 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
                         const uint32_t c = i / 64u, row = (i / 2u) % 32u, h = i % 2u;
                         const uint16_t *p = kt + row * pitch + c * 32u + h * 16u;
 #pragma unroll
-                        for (int u = 0; u < 16; ++u) w[u / 4] |= to8(widen<T>(p[u]), inv[0]) << (8 * (u % 4));
+                        for (int u = 0; u < 16; ++u) w[u / 4] |= scale[0].to8(widen<T>(p[u])) << (8 * (u % 4));
                     } else {
                         const uint32_t d = (i - 2u * dim) / 2u, h = i % 2u;
 #pragma unroll
-                        for (int u = 0; u < 16; ++u) w[u / 4] |= to8(widen<T>(vt[token_at(16u * h + u) * pitch + d]), inv[1]) << (8 * (u % 4));
+                        for (int u = 0; u < 16; ++u) w[u / 4] |= scale[1].to8(widen<T>(vt[token_at(16u * h + u) * pitch + d])) << (8 * (u % 4));
                     }
                     *reinterpret_cast<u32x4 *>(to + 16u * i) = u32x4{w[0], w[1], w[2], w[3]};
                 }
-                if (tid < 2u) a.c.scales[2u * (uint64_t)index + tid] = scale[tid];
+                if (tid < 2u) a.c.scales[2u * (uint64_t)index + tid] = tid ? scale[1].scale : scale[0].scale;
             }
         }
         if (jj + 1u >= open && (turn_no || mine)) {        // the ring: the block's new tokens
             uint8_t *half = ring_half(a.c, slot, head, jj);
             _Float16 *kr = reinterpret_cast<_Float16 *>(half), *vr = kr + 32u * dim;
             float *e = reinterpret_cast<float *>(half + 128ull * dim);
-            const uint32_t r0 = jj * kBlk < before ? before - jj * kBlk : 0u;
-            const uint32_t r1 = len - jj * kBlk < (uint32_t)kBlk ? len - jj * kBlk : (uint32_t)kBlk;
             if (tid < 64u && tid % 32u >= r0 && tid % 32u < r1) {
                 const uint32_t m = s_amax[tid / 32u][tid % 32u];
                 e[tid] = m >= kInf16<T> ? __uint_as_float(0x7fc00000u) : token_scale(widen<T>((uint16_t)m));
@@ -240,23 +355,49 @@ template <typename T>
 __global__ __launch_bounds__(kCacheBlock) void k_cache_fetch(FetchArgs a) {
     extern __shared__ __align__(16) uint16_t s_rows[];
     const uint32_t tid = threadIdx.x, unit = blockIdx.x, head = blockIdx.y, dim = a.c.dim, pitch = dim + 8u;
-    const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, 1u, 5u, 2u);
-    Seq s;
-    if (!read_sequence(a.b, seq, &s)) return;
-    const uint32_t first = first_unit(a.b.starts, seq, 1u, 5u, 2u);
-    if (unit < first) return;
-    if (s.len < s.n) {
-        raise(a.b.status);
-        return;
-    }
-    const uint32_t len = (uint32_t)s.len, before = len - (uint32_t)s.n, j = before / kBlk + (unit - first);
-    if (j > (len - 1u) / kBlk) return;
+    Unit found;
+    if (!find_block(a.b, unit, &found)) return;
+    const uint32_t seq = found.seq, j = found.block;
+    const Seq s = found.s;
+    const uint32_t len = (uint32_t)s.len, before = len - (uint32_t)s.n;
     uint16_t *kt = s_rows, *vt = s_rows + kBlk * pitch;
     if (j < len / kBlk) {
         const int64_t index = block_index(a.b, a.c, seq, head, j);
         if (index < 0) return;
         const uint8_t *from = a.c.blocks + (uint64_t)index * 64u * dim;
         const float ks = a.c.scales[2u * (uint64_t)index], vs = a.c.scales[2u * (uint64_t)index + 1u];
+        if (a.vec) {                                       // in registers, as in compress_block
+            const int32_t token0 = s.start + (int32_t)(j * kBlk) - (int32_t)before;
+            const uint32_t r0 = j * kBlk < before ? before - j * kBlk : 0u, per_row = dim / 16u;
+            for (uint32_t i = tid; i < 2u * dim; i += kCacheBlock) {
+                const uint32_t row = i / per_row, c = i - row * per_row;
+                if (row < r0) continue;
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(from + c / 2u * 1024u + row * 32u + c % 2u * 16u);
+                T *to = reinterpret_cast<T *>(a.k.p) + (int64_t)(token0 + (int32_t)row) * a.k.token + (int64_t)head * a.k.head + 16u * c;
+                float x[16];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) x[u] = (float)(int8_t)(w[u / 4] >> (8 * (u % 4))) * ks;
+                store_row<T, 8>(to, x);
+                store_row<T, 8>(to + 8, x + 8);
+            }
+            for (uint32_t i = tid; i < dim; i += kCacheBlock) {
+                const uint32_t quad = i % 8u, d = i / 8u * 8u;
+                const uint8_t *at = from + 32u * dim + 32u * d + place_of(4u * quad);
+                uint32_t w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = *reinterpret_cast<const uint32_t *>(at + 32u * k);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t row = 4u * quad + u;
+                    if (row < r0) continue;
+                    float x[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = (float)(int8_t)(w[k] >> (8 * u)) * vs;
+                    store_row<T, 8>(reinterpret_cast<T *>(a.v.p) + (int64_t)(token0 + (int32_t)row) * a.v.token + (int64_t)head * a.v.head + d, x);
+                }
+            }
+            return;
+        }
         for (uint32_t i = tid; i < 4u * dim; i += kCacheBlock) {
             const u32x4 w = *reinterpret_cast<const u32x4 *>(from + 16u * i);
             if (i < 2u * dim) {
@@ -270,15 +411,19 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_fetch(FetchArgs a) {
             }
         }
     } else {
-        uint32_t slot;
-        if (!read_slot(a.b, a.c, seq, &slot)) return;
-        const uint8_t *half = ring_half(a.c, slot, head, j);
+        if (!check_slot(a.b, a.c, found.slot)) return;
+        const uint8_t *half = ring_half(a.c, (uint32_t)found.slot, head, j);
         const uint16_t *kr = reinterpret_cast<const uint16_t *>(half), *vr = kr + 32u * dim;
         const float *e = reinterpret_cast<const float *>(half + 128ull * dim);
-        for (uint32_t i = tid; i < kBlk * dim; i += kCacheBlock) {
-            const uint32_t row = i / dim, d = i % dim;
-            kt[row * pitch + d] = narrow<T>(widen<_Float16>(kr[(d / 32u * 32u + row) * 32u + d % 32u]) * e[row]);
-            vt[row * pitch + d] = narrow<T>(widen<_Float16>(vr[d * 32u + place_of(row)]) * e[32u + row]);
+        const uint32_t r0 = j * kBlk < before ? before - j * kBlk : 0u, r1 = len - j * kBlk;        // the rows asked for
+        for (uint32_t i = tid; i < (r1 - r0) * (dim / 8u); i += kCacheBlock) {
+            const uint32_t row = r0 + i / (dim / 8u), d = i % (dim / 8u) * 8u;
+            const half8 k = *reinterpret_cast<const half8 *>(kr + (d / 32u * 32u + row) * 32u + d % 32u);
+#pragma unroll
+            for (uint32_t u = 0; u < 8u; ++u) {
+                kt[row * pitch + d + u] = narrow<T>((float)k[u] * e[row]);
+                vt[row * pitch + d + u] = narrow<T>(widen<_Float16>(vr[(d + u) * 32u + place_of(row)]) * e[32u + row]);
+            }
         }
     }
     __syncthreads();

@@ -193,6 +193,9 @@ template <int ROWS> __device__ inline uint32_t token_of(int t) {
     return 16u * (t / 4) + 4u * ((uint32_t)lane_id() >> 4) + t % 4;
 }
 
+// What rounding a weight to float16 leaves, in float16 once more.
+__device__ inline _Float16 rest_of(float w, _Float16 p) { return (_Float16)(w - (float)p); }
+
 // A row's numbers, in the lanes l with l % ROWS its number in the tile.
 template <int NO, typename ACC, int ROWS>
 struct RowState {
@@ -219,7 +222,7 @@ struct RowState {
     }
     // The weights of a block that the whole tile sees, from its raw products; kc = a c, lb = log2 b.
     template <typename S>
-    __device__ void weights(const S &s, float kc, float lb, half8 *p) {
+    __device__ void weights(const S &s, float kc, float lb, half8 *p, half8 *rest = nullptr) {
         // where b is so small that p is 0 anyway, only l counts
         const float c1 = fmaxf(lb - r + kLift, -60.0f - m);
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -228,32 +231,40 @@ struct RowState {
             const float w = exp2_fast(__builtin_fmaf(s[t], kc, c1));
             sum[t % 4] += w;
             p[t / 8][t % 8] = (_Float16)w;
+            if (rest) rest[t / 8][t % 8] = rest_of(w, (_Float16)w);
         }
         l = __builtin_fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), exp2_fast(-c1 - m), l);
     }
     // The same for a block of which rows see parts: x = -Inf elsewhere.  A poisoned block's lb is NaN, and so are the weights seen.
-    __device__ void weights_some(const float *x, float lb, half8 *p) {
+    __device__ void weights_some(const float *x, float lb, half8 *p, half8 *rest = nullptr) {
         const float ms = m == kNegInf ? 0.0f : m, c1 = lb - (r == kNegInf ? 0.0f : r) + kLift;
         float sum = 0.0f;
 #pragma unroll
         for (int t = 0; t < N; ++t) {
+            const float w = exp2_fast(x[t] + c1);
             sum += exp2_fast(x[t] - ms);
-            p[t / 8][t % 8] = (_Float16)exp2_fast(x[t] + c1);
+            p[t / 8][t % 8] = (_Float16)w;
+            if (rest) rest[t / 8][t % 8] = rest_of(w, (_Float16)w);
         }
         l += sum;
         if (lb != lb) {
 #pragma unroll
             for (int t = 0; t < N; ++t)
-                if (x[t] == kNegInf) p[t / 8][t % 8] = (_Float16)0.0f;
+                if (x[t] == kNegInf) {
+                    p[t / 8][t % 8] = (_Float16)0.0f;
+                    if (rest) rest[t / 8][t % 8] = (_Float16)0.0f;
+                }
         }
     }
     // ... and for tokens each with a scale of its own: lv = log2 b, 0 where x = -Inf.
-    __device__ void weights_each(const float *x, const float *lv, half8 *p) {
+    __device__ void weights_each(const float *x, const float *lv, half8 *p, half8 *rest = nullptr) {
         const float ms = m == kNegInf ? 0.0f : m, rs = r == kNegInf ? 0.0f : r;
 #pragma unroll
         for (int t = 0; t < N; ++t) {
+            const float w = exp2_fast(x[t] + (lv[t] - rs + kLift));
             l += exp2_fast(x[t] - ms);
-            p[t / 8][t % 8] = (_Float16)exp2_fast(x[t] + (lv[t] - rs + kLift));
+            p[t / 8][t % 8] = (_Float16)w;
+            if (rest) rest[t / 8][t % 8] = rest_of(w, (_Float16)w);
         }
     }
 };

@@ -103,7 +103,7 @@ struct AttendArgs {
 };
 template <int NC>
 __global__ void k_attend(AttendArgs a);
-template <int NC>
+template <int NC, bool EXACT>
 __global__ void k_attend_few(AttendArgs a);
 template <int NC, int RT>
 __global__ void k_attend_tile(AttendArgs a);

@@ -164,7 +164,9 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
 }
 
 // Fewer still: the same with tiles of 16 rows, half the registers and so twice the wavefronts and loads in flight.  Bound by HBM.
-template <int NC>
+// EXACT: what rounding the weights to float16 leaves is multiplied as well, for results in float16 (whose own rounding is no larger: together 1.45 times
+// the error of one; the second product hides behind the loads).
+template <int NC, bool EXACT>
 __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k_attend_few(AttendArgs a) {
     constexpr uint32_t dim = 32u * NC;
     __shared__ float s_stat[4][3][16];
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
             const float sc[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3], acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
             if (next >= 0) load(kr, next, 0u);
             const float kc = Lookup::of(look.ks, i) * qc, lb = Lookup::of(look.lb, i);
-            half8 pw[1];
+            half8 pw[1], rest[1] = {};
             // (one place that moves the references, and x once more behind it: two such places cost a hundred registers)
             const bool all = at >= 0 && (int32_t)(j * 32u + 32u) <= least && lb == lb;
             const int32_t limit = at >= 0 ? place.limit : 0;
@@ -238,17 +240,22 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
             }
             row.follow(top, tope);
             if (all) {
-                row.weights(sc, kc, lb, pw);
+                row.weights(sc, kc, lb, pw, EXACT ? rest : nullptr);
             } else {
                 float x[8];
                 some_of_block<16>(sc, kc, lb, j, limit, x, &top, &tope);
-                row.weights_some(x, lb, pw);
+                row.weights_some(x, lb, pw, EXACT ? rest : nullptr);
             }
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const auto x = __builtin_amdgcn_permlane32_swap(vr[c][0], vr[c][1], false, false), y = __builtin_amdgcn_permlane32_swap(vr[c][2], vr[c][3], false, false);
-                row.o[2 * c] = mfma(whole8(x[0], y[0]), pw[0], row.o[2 * c]);
-                row.o[2 * c + 1] = mfma(whole8(x[1], y[1]), pw[0], row.o[2 * c + 1]);
+                const half8 v0 = whole8(x[0], y[0]), v1 = whole8(x[1], y[1]);
+                row.o[2 * c] = mfma(v0, pw[0], row.o[2 * c]);
+                row.o[2 * c + 1] = mfma(v1, pw[0], row.o[2 * c + 1]);
+                if constexpr (EXACT) {
+                    row.o[2 * c] = mfma(v0, rest[0], row.o[2 * c]);
+                    row.o[2 * c + 1] = mfma(v1, rest[0], row.o[2 * c + 1]);
+                }
             }
             if (next >= 0) load(vr, next, 1u);
             at = next;
@@ -272,8 +279,8 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
             float x[8], lv[8], top, tope;
             each_of_open<16>(sc, qc, reinterpret_cast<const float *>(half + 128ull * dim), held, j, place.limit, x, lv, &top, &tope);
             row.follow(top, tope);
-            half8 pw[1];
-            row.weights_each(x, lv, pw);
+            half8 pw[1], rest[1];
+            row.weights_each(x, lv, pw, EXACT ? rest : nullptr);
 #pragma unroll
             for (int c = 0; c < 2 * NC; ++c) {
                 const uint8_t *from = half + 64u * dim + 64u * (16u * c + n) + 32u * (g & 1u) + 8u * (g >> 1);
@@ -286,6 +293,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
                         v[4 * u + i] = 16u * u + 4u * g + i < held ? part[i] : (_Float16)0.0f;
                 }
                 row.o[c] = mfma(v, pw[0], row.o[c]);
+                if constexpr (EXACT) row.o[c] = mfma(v, rest[0], row.o[c]);
             }
         }
     }
@@ -432,13 +440,21 @@ template __global__ void k_attend<5>(AttendArgs);
 template __global__ void k_attend<6>(AttendArgs);
 template __global__ void k_attend<7>(AttendArgs);
 template __global__ void k_attend<8>(AttendArgs);
-template __global__ void k_attend_few<1>(AttendArgs);
-template __global__ void k_attend_few<2>(AttendArgs);
-template __global__ void k_attend_few<3>(AttendArgs);
-template __global__ void k_attend_few<4>(AttendArgs);
-template __global__ void k_attend_few<5>(AttendArgs);
-template __global__ void k_attend_few<6>(AttendArgs);
-template __global__ void k_attend_few<7>(AttendArgs);
-template __global__ void k_attend_few<8>(AttendArgs);
+template __global__ void k_attend_few<1, false>(AttendArgs);
+template __global__ void k_attend_few<1, true>(AttendArgs);
+template __global__ void k_attend_few<2, false>(AttendArgs);
+template __global__ void k_attend_few<2, true>(AttendArgs);
+template __global__ void k_attend_few<3, false>(AttendArgs);
+template __global__ void k_attend_few<3, true>(AttendArgs);
+template __global__ void k_attend_few<4, false>(AttendArgs);
+template __global__ void k_attend_few<4, true>(AttendArgs);
+template __global__ void k_attend_few<5, false>(AttendArgs);
+template __global__ void k_attend_few<5, true>(AttendArgs);
+template __global__ void k_attend_few<6, false>(AttendArgs);
+template __global__ void k_attend_few<6, true>(AttendArgs);
+template __global__ void k_attend_few<7, false>(AttendArgs);
+template __global__ void k_attend_few<7, true>(AttendArgs);
+template __global__ void k_attend_few<8, false>(AttendArgs);
+template __global__ void k_attend_few<8, true>(AttendArgs);
 
 }  // namespace comet

@@ -19,16 +19,22 @@ namespace {
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLift = 7.0f, kSlack = 8.0f;      // log2: weights are at most 2^(kLift + kSlack) on their way into float16
 
-// Tiles of a.tile_rows rows and blocks of a sequence.
-__device__ inline uint32_t tiles_of(const AttendArgs &a, uint32_t seq) {
-    const int32_t s0 = a.b.starts[seq], s1 = a.b.starts[seq + 1], len = a.b.lens[seq];
-    if (s0 < 0 || s1 < s0 || s1 > (int32_t)a.b.n_tokens || len < 0 || len > kMaxLen) {
-        if (a.b.status) *a.b.status = COMET_ERR_FORMAT;
-        return 0u;
+// A sequence as the batch has it: tiles of a.tile_rows rows (none if its numbers make no sense, which is reported) and blocks.
+struct SeqWork {
+    Seq s;
+    uint32_t tiles, blocks;
+    __device__ void read(const AttendArgs &a, uint32_t seq) {
+        const int32_t s0 = a.b.starts[seq], s1 = a.b.starts[seq + 1], len = a.b.lens[seq];
+        const bool sane = s0 >= 0 && s1 >= s0 && s1 <= (int32_t)a.b.n_tokens && len >= 0 && len <= kMaxLen;
+        if (!sane && a.b.status) *a.b.status = COMET_ERR_FORMAT;
+        s.start = s0;
+        s.n = sane ? s1 - s0 : 0;
+        s.len = len;
+        tiles = (uint32_t)(((uint64_t)(uint32_t)s.n * a.group + a.tile_rows - 1u) >> a.tile_shift);
+        blocks = sane ? ((uint32_t)len + 31u) / 32u : 0u;
     }
-    return (uint32_t)(((uint64_t)(uint32_t)(s1 - s0) * a.group + a.tile_rows - 1u) >> a.tile_shift);
-}
-__device__ inline uint32_t blocks_of(const AttendArgs &a, uint32_t seq) { return (uint32_t)((a.b.lens[seq] + 31ll) / 32); }
+    __device__ void none() { s.start = s.n = s.len = 0; tiles = blocks = 0u; }
+};
 
 __device__ inline uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 // Sum over the wavefront, the same in every lane.
@@ -58,22 +64,21 @@ struct Piece {
 __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p) {
     __shared__ float s_sum[kAttendBlock / kWave];
     __shared__ uint32_t s_scan[kAttendBlock / kWave], s_found[6];
-    __shared__ uint32_t s_order[kSorted][3];
+    __shared__ uint32_t s_order[kSorted][6];
     const uint32_t tid = threadIdx.x, wave = tid / kWave;
     float total = 0.0f;                       // blocks of all tiles; the same sum in the same order in every workgroup
-    uint32_t tiles = 0, blocks = 0;
+    SeqWork w;
+    w.none();
     for (uint32_t b = tid; b < a.b.n_seqs; b += kAttendBlock) {
-        const uint32_t t = tiles_of(a, b), k = t ? blocks_of(a, b) : 0u;
-        float v = (float)k;
-        if (a.causal && a.wide && t) {                         // on the average a tile sees as much as its sequence's middle one
-            const float half = (float)(a.b.starts[b + 1] - a.b.starts[b]) * (1.0f / 64.0f);
+        SeqWork x;
+        x.read(a, b);
+        float v = (float)x.blocks;
+        if (a.causal && a.wide) {                              // on the average a tile sees as much as its sequence's middle one
+            const float half = (float)x.s.n * (1.0f / 64.0f);
             v = fmaxf(v - half, v * 0.5f);                     // (never less than half: a.slots counts on it)
         }
-        total += v * (float)t;
-        if (b == tid) {
-            tiles = t;
-            blocks = k;
-        }
+        total += v * (float)x.tiles;
+        if (b == tid) w = x;
     }
     total = wave_total(total);
     if (lane_id() == 0) s_sum[wave] = total;
@@ -92,49 +97,46 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
         if (wave == 0u) {
             uint32_t rank = 0;
             for (uint32_t k = 0; k < a.b.n_seqs; ++k) {
-                const uint32_t other = lane_value(blocks, (int)k);
-                rank += other > blocks || (other == blocks && k < tid);
+                const uint32_t other = lane_value(w.blocks, (int)k);
+                rank += other > w.blocks || (other == w.blocks && k < tid);
             }
             if (tid < a.b.n_seqs) {
-                s_order[rank][0] = tid;
-                s_order[rank][1] = tiles;
-                s_order[rank][2] = blocks;
+                uint32_t *o = s_order[rank];
+                o[0] = tid; o[1] = w.tiles; o[2] = w.blocks; o[3] = (uint32_t)w.s.start; o[4] = (uint32_t)w.s.n; o[5] = (uint32_t)w.s.len;
             }
         }
         __syncthreads();
         if (tid < a.b.n_seqs) {
-            whose = s_order[tid][0];
-            tiles = s_order[tid][1];
-            blocks = s_order[tid][2];
+            const uint32_t *o = s_order[tid];
+            whose = o[0]; w.tiles = o[1]; w.blocks = o[2]; w.s.start = (int32_t)o[3]; w.s.n = (int32_t)o[4]; w.s.len = (int32_t)o[5];
         }
     }
     uint32_t base = 0;
     for (uint32_t b0 = 0; b0 < a.b.n_seqs && base <= number; b0 += kAttendBlock) {
         const uint32_t b = b0 + tid;
         if (b0) {
-            tiles = b < a.b.n_seqs ? tiles_of(a, b) : 0u;
-            blocks = tiles ? blocks_of(a, b) : 0u;
+            w.none();
+            if (b < a.b.n_seqs) w.read(a, b);
         }
-        const uint32_t parts = blocks > per ? (blocks + per - 1u) / per : 1u, count = tiles * parts;
+        const uint32_t parts = w.blocks > per ? (w.blocks + per - 1u) / per : 1u, count = w.tiles * parts;
         const uint32_t incl = (uint32_t)run_scan<2>((int32_t)count, 0u, 64u);
         if (lane_id() == kWave - 1) s_scan[wave] = incl;
         __syncthreads();
         uint32_t before = base + incl - count;
 #pragma unroll
-        for (uint32_t w = 0; w < kAttendBlock / kWave; ++w) {
-            if (w < wave) before += s_scan[w];
-            base += s_scan[w];
+        for (uint32_t k = 0; k < kAttendBlock / kWave; ++k) {
+            if (k < wave) before += s_scan[k];
+            base += s_scan[k];
         }
         if (number - before < count) {
             const uint32_t local = number - before, tile = local / parts;
-            if (tile < tiles) {                                // (not so only where the batch's numbers make no sense)
+            if (tile < w.tiles) {                              // (not so only where the batch's numbers make no sense)
                 s_found[0] = sorted ? whose : b;
-                s_found[1] = a.causal ? tiles - 1u - tile : tile;      // a causal prompt's last tiles see most: they begin first
+                s_found[1] = a.causal ? w.tiles - 1u - tile : tile;    // a causal prompt's last tiles see most: they begin first
                 s_found[2] = local - tile * parts;
-                const uint32_t seq = s_found[0];
-                s_found[3] = (uint32_t)a.b.starts[seq];
-                s_found[4] = (uint32_t)(a.b.starts[seq + 1] - a.b.starts[seq]);
-                s_found[5] = (uint32_t)a.b.lens[seq];
+                s_found[3] = (uint32_t)w.s.start;
+                s_found[4] = (uint32_t)w.s.n;
+                s_found[5] = (uint32_t)w.s.len;
             }
         }
         __syncthreads();
@@ -344,24 +346,26 @@ __device__ inline float convert_query(const AttendArgs &a, const QueryRaw<NW> &r
     return scale;
 }
 
-// Where a block lies and its scales: looked up by the lanes of a wavefront, one block each.
+// Where a block lies and its scales: looked up by the lanes of a wavefront, one block each.  request() waits for the pages alone, so that what
+// lies at the index can be loaded beside the scales, which finish() waits for.
 struct Lookup {
     int64_t index;              // or -1: no such page
     float ks, lb;               // scale of the keys, log2 of the values'
+    __device__ void request(const AttendArgs &a, uint32_t seq, uint32_t head, uint32_t j, uint32_t end) {
+        const uint32_t col = j / a.c.per;
+        const bool asked = j < end, listed = asked && col < a.b.width;
+        const int32_t page = a.b.table[listed ? (uint64_t)seq * a.b.width + col : 0u];
+        const bool there = listed && page >= 0 && (uint32_t)page < a.c.n_pages;
+        index = there ? ((int64_t)page * a.c.heads + head) * a.c.per + (j - col * a.c.per) : -1;
+        if (asked && !there && a.b.status) *a.b.status = COMET_ERR_FORMAT;
+        const float *s = a.c.scales + (there ? 2 * index : 0);
+        ks = s[0];
+        lb = s[1];
+    }
+    __device__ void finish() { lb = log2_fast(lb); }
     __device__ void get(const AttendArgs &a, uint32_t seq, uint32_t head, uint32_t j, uint32_t end) {
-        index = -1;
-        ks = lb = 0.0f;
-        if (j < end) {
-            const uint32_t col = j / a.c.per;
-            const int32_t page = col < a.b.width ? a.b.table[(uint64_t)seq * a.b.width + col] : -1;
-            if (page >= 0 && (uint32_t)page < a.c.n_pages) {
-                index = ((int64_t)page * a.c.heads + head) * a.c.per + (j - col * a.c.per);
-                ks = a.c.scales[2 * index];
-                lb = log2_fast(a.c.scales[2 * index + 1]);
-            } else if (a.b.status) {
-                *a.b.status = COMET_ERR_FORMAT;
-            }
-        }
+        request(a, seq, head, j, end);
+        finish();
     }
     __device__ int64_t index_of(uint32_t i) const {
         const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(uint64_t)index, (int)i);

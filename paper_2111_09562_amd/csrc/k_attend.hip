@@ -33,20 +33,23 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
     uint32_t j = j0 + wave;
     const uint32_t end = j1 < whole ? j1 : whole;
     u32x4 kr[NC], vr[NC];
-    Lookup look;
-    look.get(a, p.seq, head, j + 4u * lane, end);
-    half8 q[2 * NC];
-    const float qc = convert_query<32>(a, raw, q) * a.scale;
-    while (j < end) {
-        const uint32_t left = (end - j + 3u) / 4u, count = left < 64u ? left : 64u;
-        const auto load = [&](u32x4 *to, int64_t at, uint32_t which) {
-            const uint8_t *from = a.c.blocks + (uint64_t)(at < 0 ? 0 : at) * (64u * dim) + which * (32u * dim) + n * 32u + h * 16u;
+    const auto load = [&](u32x4 *to, int64_t at, uint32_t which) {
+        const uint8_t *from = a.c.blocks + (uint64_t)(at < 0 ? 0 : at) * (64u * dim) + which * (32u * dim) + n * 32u + h * 16u;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) to[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024);
-        };
-        int64_t at = look.index_of(0);
+        for (int c = 0; c < NC; ++c) to[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024);
+    };
+    Lookup look;
+    look.request(a, p.seq, head, j + 4u * lane, end);
+    int64_t at = look.index_of(0);
+    if (j < end) {
         load(kr, at, 0u);
         load(vr, at, 1u);
+    }
+    half8 q[2 * NC];
+    const float qc = convert_query<32>(a, raw, q) * a.scale;
+    look.finish();
+    while (j < end) {
+        const uint32_t left = (end - j + 3u) / 4u, count = left < 64u ? left : 64u;
         for (uint32_t i = 0; i < count; ++i, j += 4u) {
             const int64_t next = i + 1u < count ? look.index_of(i + 1u) : -1;
             f32x16 acc = {};
@@ -88,7 +91,12 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
             if (next >= 0) load(vr, next, 1u);
             at = next;
         }
-        if (j < end) look.get(a, p.seq, head, j + 4u * lane, end);
+        if (j < end) {
+            look.get(a, p.seq, head, j + 4u * lane, end);
+            at = look.index_of(0);
+            load(kr, at, 0u);
+            load(vr, at, 1u);
+        }
     }
 
     // the open block, in 16 bits, with a scale for every token
@@ -195,20 +203,23 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
     uint32_t j = j0 + wave;
     const uint32_t end = j1 < whole ? j1 : whole;
     u32x4 kr[NC], vr[NC];
-    Lookup look;
-    look.get(a, p.seq, head, j + 4u * lane, end);
-    half8 q[NC];
-    const float qc = convert_query<16>(a, raw, q) * a.scale;
-    while (j < end) {
-        const uint32_t left = (end - j + 3u) / 4u, count = left < 64u ? left : 64u;
-        const auto load = [&](u32x4 *to, int64_t at, uint32_t which) {
-            const uint8_t *from = a.c.blocks + (uint64_t)(at < 0 ? 0 : at) * (64u * dim) + which * (32u * dim) + n * 32u + (g >> 1) * 512u + (g & 1u) * 16u;
+    const auto load = [&](u32x4 *to, int64_t at, uint32_t which) {
+        const uint8_t *from = a.c.blocks + (uint64_t)(at < 0 ? 0 : at) * (64u * dim) + which * (32u * dim) + n * 32u + (g >> 1) * 512u + (g & 1u) * 16u;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) to[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024);
-        };
-        int64_t at = look.index_of(0);
+        for (int c = 0; c < NC; ++c) to[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024);
+    };
+    Lookup look;
+    look.request(a, p.seq, head, j + 4u * lane, end);
+    int64_t at = look.index_of(0);
+    if (j < end) {
         load(kr, at, 0u);
         load(vr, at, 1u);
+    }
+    half8 q[NC];
+    const float qc = convert_query<16>(a, raw, q) * a.scale;
+    look.finish();
+    while (j < end) {
+        const uint32_t left = (end - j + 3u) / 4u, count = left < 64u ? left : 64u;
         for (uint32_t i = 0; i < count; ++i, j += 4u) {
             const int64_t next = i + 1u < count ? look.index_of(i + 1u) : -1;
             // Lane l has loaded 16 values of one token (l & 15, 16 more in the upper half of the wavefront), the instruction wants eight of the token
@@ -260,7 +271,12 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
             if (next >= 0) load(vr, next, 1u);
             at = next;
         }
-        if (j < end) look.get(a, p.seq, head, j + 4u * lane, end);
+        if (j < end) {
+            look.get(a, p.seq, head, j + 4u * lane, end);
+            at = look.index_of(0);
+            load(kr, at, 0u);
+            load(vr, at, 1u);
+        }
     }
 
     // the open block, in 16 bits, with a scale for every token
@@ -353,15 +369,17 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_join(AttendArgs a) {
     const uint32_t unit = blockIdx.x / a.c.heads, head = blockIdx.x - unit * a.c.heads;
     const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, a.group, a.tile_shift, 1u);
     const uint32_t first = first_unit(a.b.starts, seq, a.group, a.tile_shift, 1u);
-    const uint32_t tile = unit - first, tiles = tiles_of(a, seq);
+    SeqWork w;
+    w.read(a, seq);
+    const uint32_t tile = unit - first, tiles = w.tiles;
     if (unit < first || tile >= tiles) return;
     const uint32_t number = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
     if (parts < 2u || number >= a.slots || parts > a.slots - number) return;   // (starts that make no sense leave entries unwritten)
-    const uint32_t rows = (uint32_t)(a.b.starts[seq + 1] - a.b.starts[seq]) * a.group;
+    const uint32_t rows = (uint32_t)w.s.n * a.group;
     const uint32_t quads = dim / 4u, lots = kAttendBlock / quads, lot = tid / quads, quad = tid - lot * quads;    // lots: pieces at a time
     for (uint32_t n = blockIdx.y; n < a.tile_rows && tile * a.tile_rows + n < rows; n += gridDim.y) {
         const uint32_t row = tile * a.tile_rows + n, query = row / a.group, qh = head * a.group + (row - query * a.group);
-        const int64_t token = (int64_t)a.b.starts[seq] + query;
+        const int64_t token = (int64_t)w.s.start + query;
         const auto slot = [&](uint32_t k) { return ((uint64_t)(number + k) * a.c.heads + head) * a.tile_rows + n; };
         float m = kNegInf, r = kNegInf;
         for (uint32_t k = lane; k < parts; k += kWave) {                       // every wavefront for itself
@@ -402,11 +420,13 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_join_tile(AttendArgs a)
     const uint32_t unit = blockIdx.x / a.c.heads, head = blockIdx.x - unit * a.c.heads;
     const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, a.group, a.tile_shift, 1u);
     const uint32_t first = first_unit(a.b.starts, seq, a.group, a.tile_shift, 1u);
-    const uint32_t tile = unit - first, tiles = tiles_of(a, seq);
+    SeqWork w;
+    w.read(a, seq);
+    const uint32_t tile = unit - first, tiles = w.tiles;
     if (unit < first || tile >= tiles) return;
     const uint32_t number = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
     if (parts < 2u || number >= a.slots || parts > a.slots - number) return;
-    const uint32_t rows = (uint32_t)(a.b.starts[seq + 1] - a.b.starts[seq]) * a.group;
+    const uint32_t rows = (uint32_t)w.s.n * a.group;
     for (uint32_t n = blockIdx.y * 4u + threadIdx.x / kWave; n < a.tile_rows && tile * a.tile_rows + n < rows; n += 4u * gridDim.y) {
         const uint32_t row = tile * a.tile_rows + n, query = row / a.group, qh = head * a.group + (row - query * a.group);
         const auto slot = [&](uint32_t k) { return ((uint64_t)(number + k) * a.c.heads + head) * a.tile_rows + n; };
@@ -426,7 +446,7 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_join_tile(AttendArgs a)
         const float ms = m == kNegInf ? 0.0f : m, rs = r == kNegInf ? 0.0f : r;
         const float fin = l == 0.0f ? 0.0f : exp2_fast(rs - ms - kLift) / l;
         RowPlace p;
-        p.real = true; p.qh = qh; p.token = (int64_t)a.b.starts[seq] + query; p.limit = 0;
+        p.real = true; p.qh = qh; p.token = (int64_t)w.s.start + query; p.limit = 0;
         if (lane == 0u && a.lse) a.lse[p.token * a.q_heads + qh] = log_sum(ms, l);
         if (4u * lane < dim) store_out(a, p, 4u * lane, o * fin);
     }

@@ -137,6 +137,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
             half8 kk[2 * NC], vv[2 * NC], pa[2] = {}, pb[2] = {};
             operands(kk, 0, 0);
             f32x16 sa = products(kk, 0), sb = {};
+            if constexpr (RT == 1) operands(kk, 0, 1);
 #pragma unroll
             for (int c = 0; c < 2 * NC; ++c) vv[c] = half8{};
             for (; i < n_fast; ++i) {
@@ -171,16 +172,17 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
                     row[1].weights(sb, kd, lb, pb);
                     if constexpr (!tile_pairs(NC, RT)) interleave<4 * NC, 20 / NC>(pb, row[1].l);
                 } else {
-                    operands(kk, 0, buf ^ 1u);
+                    operands(vv, 1, buf);
                     sb = products(kk, 0);
                     row[0].weights(sa, kc, lb, pa);
                     if constexpr (!tile_pairs(NC, RT)) interleave<2 * NC, 32 / NC>(pa, row[0].l);
-                    operands(vv, 1, buf);
                     next();
+                    __syncthreads();
+                    operands(kk, 0, buf);                                  // of block i + 2, while the values are multiplied
                     accumulate(vv, 0, pa);
                     sa = sb;
                 }
-                __syncthreads();
+                if constexpr (RT == 2) __syncthreads();
             }
             if constexpr (RT == 2) accumulate(vv, 1, pb);
         }

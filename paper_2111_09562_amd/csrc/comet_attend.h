@@ -54,7 +54,7 @@ constexpr uint32_t kSorted = 32;                   // sequences that are put in 
 struct Piece {
     uint32_t seq, tile, part;
     uint32_t per;                         // blocks of a part
-    uint32_t number;                      // among all pieces of a head
+    uint32_t slot;                        // among the pieces of tiles that are cut: where its results go
     Seq s;
 };
 // Cuts the blocks of all tiles into pieces of the same length, so that sequences of very different lengths keep all compute units
@@ -63,7 +63,7 @@ struct Piece {
 // read for those beyond 256); ends the same way for all threads.
 __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p) {
     __shared__ float s_sum[kAttendBlock / kWave];
-    __shared__ uint32_t s_scan[kAttendBlock / kWave], s_found[6];
+    __shared__ uint32_t s_scan[kAttendBlock / kWave][2], s_found[7];
     __shared__ uint32_t s_order[kSorted][6];
     const uint32_t tid = threadIdx.x, wave = tid / kWave;
     float total = 0.0f;                       // blocks of all tiles; the same sum in the same order in every workgroup
@@ -75,7 +75,7 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
         float v = (float)x.blocks;
         if (a.causal && a.wide) {                              // on the average a tile sees as much as its sequence's middle one
             const float half = (float)x.s.n * (1.0f / 64.0f);
-            v = fmaxf(v - half, v * 0.5f);                     // (never less than half: a.slots counts on it)
+            v = fmaxf(v - half, v * 0.5f);                     // (never less than half: the grid counts on it)
         }
         total += v * (float)x.tiles;
         if (b == tid) w = x;
@@ -86,7 +86,7 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
     __syncthreads();
     total = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
     // an eighth more than the average (a tile that is just longer than that is not worth a second piece), which also keeps what float32
-    // rounds from making more pieces than there are slots
+    // rounds from making more pieces than the grid has
     const float most = __builtin_ceilf(total * 1.125f / (float)a.pieces);
     uint32_t per = most < 2147483000.0f ? (uint32_t)most : 2147483000u;
     if (per < a.min_blocks) per = a.min_blocks;
@@ -111,7 +111,7 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
             whose = o[0]; w.tiles = o[1]; w.blocks = o[2]; w.s.start = (int32_t)o[3]; w.s.n = (int32_t)o[4]; w.s.len = (int32_t)o[5];
         }
     }
-    uint32_t base = 0;
+    uint32_t base = 0, cut_base = 0;
     for (uint32_t b0 = 0; b0 < a.b.n_seqs && base <= number; b0 += kAttendBlock) {
         const uint32_t b = b0 + tid;
         if (b0) {
@@ -119,14 +119,22 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
             if (b < a.b.n_seqs) w.read(a, b);
         }
         const uint32_t parts = w.blocks > per ? (w.blocks + per - 1u) / per : 1u, count = w.tiles * parts;
-        const uint32_t incl = (uint32_t)run_scan<2>((int32_t)count, 0u, 64u);
-        if (lane_id() == kWave - 1) s_scan[wave] = incl;
+        const uint32_t cut = parts > 1u ? count : 0u;
+        const uint32_t incl = (uint32_t)run_scan<2>((int32_t)count, 0u, 64u), cut_incl = (uint32_t)run_scan<2>((int32_t)cut, 0u, 64u);
+        if (lane_id() == kWave - 1) {
+            s_scan[wave][0] = incl;
+            s_scan[wave][1] = cut_incl;
+        }
         __syncthreads();
-        uint32_t before = base + incl - count;
+        uint32_t before = base + incl - count, cut_before = cut_base + cut_incl - cut;
 #pragma unroll
         for (uint32_t k = 0; k < kAttendBlock / kWave; ++k) {
-            if (k < wave) before += s_scan[k];
-            base += s_scan[k];
+            if (k < wave) {
+                before += s_scan[k][0];
+                cut_before += s_scan[k][1];
+            }
+            base += s_scan[k][0];
+            cut_base += s_scan[k][1];
         }
         if (number - before < count) {
             const uint32_t local = number - before, tile = local / parts;
@@ -137,6 +145,7 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
                 s_found[3] = (uint32_t)w.s.start;
                 s_found[4] = (uint32_t)w.s.n;
                 s_found[5] = (uint32_t)w.s.len;
+                s_found[6] = cut_before + local;
             }
         }
         __syncthreads();
@@ -145,7 +154,7 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
     p->tile = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_found[1]);
     p->part = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_found[2]);
     p->per = (uint32_t)__builtin_amdgcn_readfirstlane((int)per);
-    p->number = number;
+    p->slot = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_found[6]);
     p->s.start = __builtin_amdgcn_readfirstlane((int)s_found[3]);
     p->s.n = __builtin_amdgcn_readfirstlane((int)s_found[4]);
     p->s.len = __builtin_amdgcn_readfirstlane((int)s_found[5]);

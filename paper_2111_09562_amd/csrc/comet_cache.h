@@ -95,11 +95,11 @@ struct AttendArgs {
     uint32_t tile_rows, tile_shift;           // rows of a workgroup: 2^tile_shift
     uint32_t min_blocks;                      // of a piece
     uint32_t pieces;                          // pieces the work of a key/value head is cut into, about
-    uint32_t slots;                           // pieces there are at most
+    uint32_t slots;                           // pieces of tiles that are cut, per head, at most
     float scale;                              // of the scores, times log2(e)
     float *part_o;                            // [slot][head][tile_rows][dim]
     float *part_s;                            // [slot][head][tile_rows][3]: reference and sum of the weights, reference of the values
-    int32_t *directory;                       // [tile][2]: first piece, number of pieces
+    int32_t *directory;                       // [tile][2]: first slot, number of pieces
 };
 template <int NC>
 __global__ void k_attend(AttendArgs a);

@@ -16,8 +16,8 @@ namespace {
         if (e_ != hipSuccess) return hip_fail(e_, #expr);               \
     } while (0)
 
-constexpr uint32_t kMaxHeads = 4096, kMaxQueryHeads = 16384, kMaxSeqs = 1u << 24, kMaxRopeDim = 4096;
-constexpr uint64_t kMaxRows = 0x7fffffffull;
+constexpr uint32_t kMaxHeads = 4096, kMaxQueryHeads = 16384, kMaxSeqs = 1u << 22, kMaxRopeDim = 4096;
+constexpr uint64_t kMaxRows = 0x7fffffffull, kMaxGroups = 0xffffffull;        // workgroups of 256: fewer than 2^32 threads
 
 bool valid_shape(comet_cache_shape s) {
     return s.n_pages && s.n_pages <= 0x7fffffffu && s.page_tokens && s.page_tokens % kBlk == 0u && s.page_tokens <= (1u << 20) && s.n_slots &&
@@ -43,7 +43,7 @@ bool cache_args(const void *dev, comet_cache_shape s, CacheArgs *c) {
     return true;
 }
 bool batch_args(const comet_cache_batch *b, uint32_t n_tokens, int32_t *status, BatchArgs *a) {
-    if (!b || b->n_seqs > kMaxSeqs || n_tokens > kMaxRows) return false;
+    if (!b || b->n_seqs > kMaxSeqs || n_tokens > kMaxRows || (uint64_t)n_tokens / kBlk + 2ull * b->n_seqs > kMaxGroups) return false;
     if (n_tokens && (!b->n_seqs || !b->table_width || !b->dev_starts || !b->dev_lens || !b->dev_table)) return false;
     for (const void *p : {(const void *)b->dev_starts, (const void *)b->dev_lens, (const void *)b->dev_table, (const void *)b->dev_slots, (const void *)status})
         if ((uintptr_t)p % 4u) return false;
@@ -57,6 +57,11 @@ bool rows_args(comet_rows r, int dtype, Rows *to) {
     to->p = static_cast<uint8_t *>(r.dev); to->token = r.token_stride; to->head = r.head_stride;
     return true;
 }
+// Rows that are written: no two of them may overlap.
+bool out_args(comet_rows r, int dtype, uint32_t tokens, uint32_t heads, uint32_t dim, Rows *to) {
+    const auto apart = [dim](int64_t stride) { return stride >= (int64_t)dim || stride <= -(int64_t)dim; };
+    return rows_args(r, dtype, to) && (tokens < 2u || apart(r.token_stride)) && (heads < 2u || apart(r.head_stride));
+}
 bool rows_aligned(const Rows &r, int dtype) {                                   // every row begins at a multiple of 16 bytes
     const int64_t v = 16 / elem_size(dtype);
     return (uintptr_t)r.p % 16u == 0u && r.token % v == 0 && r.head % v == 0;
@@ -69,7 +74,7 @@ bool rope_args(const comet_rope_plan *p, uint32_t dim, const int32_t *positions,
     r->steps = p->dev_steps; r->positions = positions; r->rot = p->rot; r->interleaved = p->layout == COMET_ROPE_PAIRS; r->amp = p->amp;
     return true;
 }
-inline uint32_t block_units(const BatchArgs &b) { return b.n_tokens / kBlk + 2u * b.n_seqs; }      // < 2^26 + 2^25 (first_unit)
+inline uint32_t block_units(const BatchArgs &b) { return b.n_tokens / kBlk + 2u * b.n_seqs; }      // (first_unit)
 
 template <typename T, int V>
 void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tokens, uint32_t heads, uint32_t dim, bool in_place, uint32_t sign, hipStream_t st) {
@@ -83,7 +88,8 @@ void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tok
     g.groups = (uint32_t)((heads + per - 1u) / per);
     g.per_token = g.groups * g.chunks;
     g.tokens_wg = g.per_token <= (uint32_t)kRopeBlock ? kRopeBlock / g.per_token : 0u;
-    const uint32_t wg = g.tokens_wg ? (n_tokens - 1u) / g.tokens_wg + 1u : n_tokens;
+    uint32_t wg = g.tokens_wg ? (n_tokens - 1u) / g.tokens_wg + 1u : n_tokens;
+    if (wg > kMaxGroups) wg = kMaxGroups;
     k_rope<T, V><<<wg, kRopeBlock, 0, st>>>(r, g, x, y, n_tokens, heads, dim, sign);
 }
 
@@ -93,7 +99,7 @@ void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tok
 // with 512, 153 with 768).
 constexpr uint32_t kAttendPieces = 768, kAttendPiecesLong = 512, kAttendTilePieces = 512;
 struct AttendPlan {
-    uint32_t pieces, slots, tiles, tile_shift, min_blocks;
+    uint32_t pieces, grid, slots, tiles, tile_shift, min_blocks;
     bool few, wide, two;                                 // k_attend_few; k_attend_tile; that with two tiles of 32 rows per wavefront
     uint64_t off_s, off_dir, bytes;
 };
@@ -110,10 +116,12 @@ bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32
     p->tiles = (uint32_t)(rows >> p->tile_shift) + n_seqs;
     p->pieces = ((p->wide ? kAttendTilePieces : (uint64_t)p->tiles * s.heads < 128u ? kAttendPiecesLong : kAttendPieces) + s.heads - 1u) / s.heads;
     p->min_blocks = p->wide ? 16u : 4u;
-    // a tile's pieces are counted as if it saw all of its sequence: of tiles of a causal prompt up to half have nothing to do
-    p->slots = (p->wide ? 2u : 1u) * p->pieces + p->tiles;
-    const uint64_t n = (uint64_t)p->slots * s.heads, per = 1ull << p->tile_shift;
-    if (n > kMaxRows) return false;
+    // A tile's pieces are counted as if it saw all of its sequence: of tiles of a causal prompt up to half have nothing to do.  Tiles that are cut
+    // have more than total / pieces blocks, so there are at most `pieces` of them (twice that), each with one piece more than its share.
+    const uint64_t most = (p->wide ? 2u : 1u) * (uint64_t)p->pieces, grid = (most + p->tiles) * s.heads, n = (uint64_t)(2u * most) * s.heads, per = 1ull << p->tile_shift;
+    if (grid > kMaxGroups) return false;
+    p->grid = (uint32_t)grid;
+    p->slots = (uint32_t)(2u * most);
     p->off_s = n * per * s.dim * 4u;
     p->off_dir = p->off_s + n * per * 3u * 4u;
     p->bytes = p->off_dir + 8ull * (p->tiles + 1ull);
@@ -174,7 +182,7 @@ int comet_rope(const comet_rope_plan *plan, comet_rows x, comet_rows y, uint32_t
     if (!plan || dtype < COMET_F32 || dtype > COMET_BF16 || !heads || heads > kMaxQueryHeads || dim > kMaxRopeDim || n_tokens > kMaxRows ||
         !rope_args(plan, dim, dev_positions, &r)) return COMET_ERR_INVALID;
     if (!n_tokens) return COMET_OK;
-    if (!rows_args(x, dtype, &rx) || !rows_args(y, dtype, &ry)) return COMET_ERR_INVALID;
+    if (!rows_args(x, dtype, &rx) || !out_args(y, dtype, n_tokens, heads, dim, &ry)) return COMET_ERR_INVALID;
     const bool in_place = x.dev == y.dev;
     if (in_place && (x.token_stride != y.token_stride || x.head_stride != y.head_stride)) return COMET_ERR_INVALID;
     const uint32_t v = 16u / elem_size(dtype);
@@ -213,7 +221,7 @@ int comet_cache_append(void *dev_cache, comet_cache_shape shape, const comet_cac
     a.q_heads = q_heads;
     uint32_t q_wg = 0;
     if (q_heads) {
-        if (!rows_args(q, dtype, &a.q) || !rows_args(q_out, dtype, &a.q_out)) return COMET_ERR_INVALID;
+        if (!rows_args(q, dtype, &a.q) || !out_args(q_out, dtype, n_tokens, q_heads, shape.dim, &a.q_out)) return COMET_ERR_INVALID;
         if (q.dev == q_out.dev && (q.token_stride != q_out.token_stride || q.head_stride != q_out.head_stride)) return COMET_ERR_INVALID;
         a.vec = a.vec && rows_aligned(a.q, dtype) && rows_aligned(a.q_out, dtype);
         a.q_heads_wg = 8u;
@@ -233,7 +241,7 @@ int comet_cache_fetch(const void *dev_cache, comet_cache_shape shape, const come
     if ((dtype != COMET_F16 && dtype != COMET_BF16) || !cache_args(dev_cache, shape, &a.c) || !batch_args(batch, n_tokens, dev_status, &a.b))
         return COMET_ERR_INVALID;
     if (!n_tokens) return COMET_OK;
-    if (!rows_args(k, dtype, &a.k) || !rows_args(v, dtype, &a.v)) return COMET_ERR_INVALID;
+    if (!out_args(k, dtype, n_tokens, shape.heads, shape.dim, &a.k) || !out_args(v, dtype, n_tokens, shape.heads, shape.dim, &a.v)) return COMET_ERR_INVALID;
     a.vec = rows_aligned(a.k, dtype) && rows_aligned(a.v, dtype);
     const dim3 grid(block_units(a.b), shape.heads);
     hipStream_t st = (hipStream_t)stream;
@@ -257,7 +265,7 @@ int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const com
         !std::isfinite(scale * 1.4426950408889634f) || scale < 0.0f || (uintptr_t)dev_lse % 4u || !plan_attend(shape, batch->n_seqs, n_tokens, q_heads, &p))
         return COMET_ERR_INVALID;
     if (!n_tokens) return COMET_OK;
-    if (!rows_args(q, dtype, &a.q) || !rows_args(out, dtype, &a.out) || !dev_work || (uintptr_t)dev_work % 16u) return COMET_ERR_INVALID;
+    if (!rows_args(q, dtype, &a.q) || !out_args(out, dtype, n_tokens, q_heads, shape.dim, &a.out) || !dev_work || (uintptr_t)dev_work % 16u) return COMET_ERR_INVALID;
     if (work_bytes < p.bytes) return COMET_ERR_NOMEM;
     a.lse = dev_lse; a.q_heads = q_heads; a.group = q_heads / shape.heads;
     a.bf16 = dtype == COMET_BF16; a.causal = causal != 0; a.wide = p.wide; a.vec = rows_aligned(a.q, dtype) && rows_aligned(a.out, dtype);
@@ -268,7 +276,7 @@ int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const com
     a.part_s = reinterpret_cast<float *>(w + p.off_s);
     a.directory = reinterpret_cast<int32_t *>(w + p.off_dir);
     hipStream_t st = (hipStream_t)stream;
-    const uint32_t wg = p.slots * shape.heads;
+    const uint32_t wg = p.grid;
     switch (shape.dim / 32u) {
         case 1: launch_attend<1>(a, p, wg, st); break;
         case 2: launch_attend<2>(a, p, wg, st); break;

@@ -5,7 +5,7 @@ namespace comet {
 
 // Few rows: a wavefront holds 32 rows (queries of one key/value head, its group's heads side by side) and goes through every fourth
 // block of its workgroup's piece straight from memory into the operands of the matrix instruction, with no LDS and no barrier
-// in the loop.  Bound by HBM as long as rows are few.  grid: heads * a.slots workgroups of kAttendBlock threads, the heads of a piece side by side
+// in the loop.  Bound by HBM as long as rows are few.  grid: heads * pieces workgroups of kAttendBlock threads, the heads of a piece side by side
 template <int NC>
 __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(AttendArgs a) {
     constexpr uint32_t dim = 32u * NC;
@@ -20,7 +20,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
     int32_t least, most;
     row_limits(a, s, p.tile * 32u, 32u, &least, &most);
     const uint32_t seen = most > 0 ? ((uint32_t)most + 31u) / 32u : 0u, parts = parts_of(seen, p.per);
-    if (p.part >= parts) return;
+    if (p.part >= parts || (parts > 1u && p.slot >= a.slots)) return;     // (more slots than there are: numbers that make no sense)
     const uint32_t j0 = (uint32_t)((uint64_t)seen * p.part / parts), j1 = (uint32_t)((uint64_t)seen * (p.part + 1u) / parts);
     const uint32_t whole = (uint32_t)s.len / 32u;                                             // complete blocks
 
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
     for (int w = 0; w < 4; ++w) ll += s_stat[w][1][n] * exp2_fast(s_stat[w][0][n] - mms);
     const float mine = exp2_fast(row.r - rrs);
     const bool last = parts == 1u;
-    const uint64_t slot_no = ((uint64_t)p.number * a.c.heads + head) * 32u;
+    const uint64_t slot_no = ((uint64_t)p.slot * a.c.heads + head) * 32u;
     if (wave == 0u && h == 0u) {
         if (last) {
             if (place.real && a.lse) a.lse[place.token * a.q_heads + place.qh] = log_sum(mms, ll);
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
         }
         if (p.part == 0u && head == 0u && n == 0u) {
             int32_t *dir = a.directory + 2u * (first_unit(a.b.starts, p.seq, a.group, a.tile_shift, 1u) + p.tile);
-            dir[0] = (int32_t)p.number;
+            dir[0] = (int32_t)p.slot;
             dir[1] = (int32_t)parts;
         }
     }
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
     int32_t least, most;
     row_limits(a, s, p.tile * 16u, 16u, &least, &most);
     const uint32_t seen = most > 0 ? ((uint32_t)most + 31u) / 32u : 0u, parts = parts_of(seen, p.per);
-    if (p.part >= parts) return;
+    if (p.part >= parts || (parts > 1u && p.slot >= a.slots)) return;     // (more slots than there are: numbers that make no sense)
     const uint32_t j0 = (uint32_t)((uint64_t)seen * p.part / parts), j1 = (uint32_t)((uint64_t)seen * (p.part + 1u) / parts);
     const uint32_t whole = (uint32_t)s.len / 32u;                                             // complete blocks
 
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
     for (int w = 0; w < 4; ++w) ll += s_stat[w][1][n] * exp2_fast(s_stat[w][0][n] - mms);
     const float mine = exp2_fast(row.r - rrs);
     const bool last = parts == 1u;
-    const uint64_t slot_no = ((uint64_t)p.number * a.c.heads + head) * 16u;
+    const uint64_t slot_no = ((uint64_t)p.slot * a.c.heads + head) * 16u;
     if (wave == 0u && g == 0u) {
         if (last) {
             if (place.real && a.lse) a.lse[place.token * a.q_heads + place.qh] = log_sum(mms, ll);
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
         }
         if (p.part == 0u && head == 0u && n == 0u) {
             int32_t *dir = a.directory + 2u * (first_unit(a.b.starts, p.seq, a.group, a.tile_shift, 1u) + p.tile);
-            dir[0] = (int32_t)p.number;
+            dir[0] = (int32_t)p.slot;
             dir[1] = (int32_t)parts;
         }
     }
@@ -373,14 +373,14 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_join(AttendArgs a) {
     w.read(a, seq);
     const uint32_t tile = unit - first, tiles = w.tiles;
     if (unit < first || tile >= tiles) return;
-    const uint32_t number = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
-    if (parts < 2u || number >= a.slots || parts > a.slots - number) return;   // (starts that make no sense leave entries unwritten)
+    const uint32_t slot0 = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
+    if (parts < 2u || slot0 >= a.slots || parts > a.slots - slot0) return;   // (starts that make no sense leave entries unwritten)
     const uint32_t rows = (uint32_t)w.s.n * a.group;
     const uint32_t quads = dim / 4u, lots = kAttendBlock / quads, lot = tid / quads, quad = tid - lot * quads;    // lots: pieces at a time
     for (uint32_t n = blockIdx.y; n < a.tile_rows && tile * a.tile_rows + n < rows; n += gridDim.y) {
         const uint32_t row = tile * a.tile_rows + n, query = row / a.group, qh = head * a.group + (row - query * a.group);
         const int64_t token = (int64_t)w.s.start + query;
-        const auto slot = [&](uint32_t k) { return ((uint64_t)(number + k) * a.c.heads + head) * a.tile_rows + n; };
+        const auto slot = [&](uint32_t k) { return ((uint64_t)(slot0 + k) * a.c.heads + head) * a.tile_rows + n; };
         float m = kNegInf, r = kNegInf;
         for (uint32_t k = lane; k < parts; k += kWave) {                       // every wavefront for itself
             const float *st = a.part_s + 3u * slot(k);
@@ -424,12 +424,12 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_join_tile(AttendArgs a)
     w.read(a, seq);
     const uint32_t tile = unit - first, tiles = w.tiles;
     if (unit < first || tile >= tiles) return;
-    const uint32_t number = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
-    if (parts < 2u || number >= a.slots || parts > a.slots - number) return;
+    const uint32_t slot0 = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
+    if (parts < 2u || slot0 >= a.slots || parts > a.slots - slot0) return;
     const uint32_t rows = (uint32_t)w.s.n * a.group;
     for (uint32_t n = blockIdx.y * 4u + threadIdx.x / kWave; n < a.tile_rows && tile * a.tile_rows + n < rows; n += 4u * gridDim.y) {
         const uint32_t row = tile * a.tile_rows + n, query = row / a.group, qh = head * a.group + (row - query * a.group);
-        const auto slot = [&](uint32_t k) { return ((uint64_t)(number + k) * a.c.heads + head) * a.tile_rows + n; };
+        const auto slot = [&](uint32_t k) { return ((uint64_t)(slot0 + k) * a.c.heads + head) * a.tile_rows + n; };
         float m = kNegInf, r = kNegInf, l = 0.0f;
         f32x4 o = {};
         for (uint32_t k = 0; k < parts; ++k) {

@@ -37,7 +37,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
     int32_t least, most;
     row_limits(a, s, p.tile * rows_wg, rows_wg, &least, &most);
     const uint32_t seen = most > 0 ? ((uint32_t)most + 31u) / 32u : 0u, parts = parts_of(seen, p.per);
-    if (p.part >= parts) return;
+    if (p.part >= parts || (parts > 1u && p.slot >= a.slots)) return;     // (more slots than there are: numbers that make no sense)
     const uint32_t j0 = (uint32_t)((uint64_t)seen * p.part / parts), j1 = (uint32_t)((uint64_t)seen * (p.part + 1u) / parts);
     const uint32_t whole = (uint32_t)s.len / 32u;
     const uint32_t row0 = p.tile * rows_wg + wave * rows_wave;
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
 
     if (p.part == 0u && head == 0u && threadIdx.x == 0u) {
         int32_t *dir = a.directory + 2u * (first_unit(a.b.starts, p.seq, a.group, a.tile_shift, 1u) + p.tile);
-        dir[0] = (int32_t)p.number;
+        dir[0] = (int32_t)p.slot;
         dir[1] = (int32_t)parts;
     }
 #pragma unroll
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
                                   f32x4{r.o[c][4 * t] * fin, r.o[c][4 * t + 1] * fin, r.o[c][4 * t + 2] * fin, r.o[c][4 * t + 3] * fin});
             }
         } else if (place[rt].real) {
-            const uint64_t slot_no = ((uint64_t)p.number * a.c.heads + head) * rows_wg + wave * rows_wave + 32u * rt + n;
+            const uint64_t slot_no = ((uint64_t)p.slot * a.c.heads + head) * rows_wg + wave * rows_wave + 32u * rt + n;
             if (h == 0u) {
                 float *st = a.part_s + 3u * slot_no;
                 st[0] = r.m; st[1] = l; st[2] = r.r;

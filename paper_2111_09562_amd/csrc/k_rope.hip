@@ -9,34 +9,35 @@ __global__ __launch_bounds__(kRopeBlock) void k_rope(RopeArgs r, RopeGrid g, Row
                                                      uint32_t sign) {
     const uint32_t tid = threadIdx.x;
     const uint32_t local = g.tokens_wg ? tid / g.per_token : 0u;
-    const uint32_t token = blockIdx.x * (g.tokens_wg ? g.tokens_wg : 1u) + local;
-    if (token >= n_tokens || (g.tokens_wg && local >= g.tokens_wg)) return;
-    const int32_t position = r.positions ? r.positions[token] : (int32_t)token;
-    const T *px = reinterpret_cast<const T *>(x.p) + (int64_t)token * x.token;
-    T *py = reinterpret_cast<T *>(y.p) + (int64_t)token * y.token;
-    for (uint32_t i = tid - local * g.per_token; i < g.per_token; i += kRopeBlock) {
-        const uint32_t group = i / g.chunks, c = i - group * g.chunks;
-        if (c < g.rot_chunks) {
-            float sn[V], cs[V];
-            chunk_angles<V>(r, c, position, sign, sn, cs);
-            const uint32_t at = chunk_at<V>(r, c), second = at + chunk_second<V>(r);
-            for (uint32_t h = group; h < heads; h += g.groups) {
-                float a[V], b[V];
-                load_row<T, V>(a, px + h * x.head + at);
-                load_row<T, V>(b, px + h * x.head + second);
-                chunk_turn<V>(r.interleaved, a, b, sn, cs);
-                store_row<T, V>(py + h * y.head + at, a);
-                store_row<T, V>(py + h * y.head + second, b);
-            }
-        } else {
-            const uint32_t at = r.rot + (c - g.rot_chunks) * V;
-            for (uint32_t h = group; h < heads; h += g.groups) {
-                float a[V];
-                load_row<T, V>(a, px + h * x.head + at);
-                store_row<T, V>(py + h * y.head + at, a);
+    const uint32_t tokens_wg = g.tokens_wg ? g.tokens_wg : 1u;
+    if (local >= tokens_wg) return;
+    for (uint64_t token = (uint64_t)blockIdx.x * tokens_wg + local; token < n_tokens; token += (uint64_t)gridDim.x * tokens_wg) {
+        const int32_t position = r.positions ? r.positions[token] : (int32_t)token;
+        const T *px = reinterpret_cast<const T *>(x.p) + (int64_t)token * x.token;
+        T *py = reinterpret_cast<T *>(y.p) + (int64_t)token * y.token;
+        for (uint32_t i = tid - local * g.per_token; i < g.per_token; i += g.tokens_wg ? g.per_token : (uint32_t)kRopeBlock) {
+            const uint32_t group = i / g.chunks, c = i - group * g.chunks;
+            if (c < g.rot_chunks) {
+                float sn[V], cs[V];
+                chunk_angles<V>(r, c, position, sign, sn, cs);
+                const uint32_t at = chunk_at<V>(r, c), second = at + chunk_second<V>(r);
+                for (uint32_t h = group; h < heads; h += g.groups) {
+                    float a[V], b[V];
+                    load_row<T, V>(a, px + h * x.head + at);
+                    load_row<T, V>(b, px + h * x.head + second);
+                    chunk_turn<V>(r.interleaved, a, b, sn, cs);
+                    store_row<T, V>(py + h * y.head + at, a);
+                    store_row<T, V>(py + h * y.head + second, b);
+                }
+            } else {
+                const uint32_t at = r.rot + (c - g.rot_chunks) * V;
+                for (uint32_t h = group; h < heads; h += g.groups) {
+                    float a[V];
+                    load_row<T, V>(a, px + h * x.head + at);
+                    store_row<T, V>(py + h * y.head + at, a);
+                }
             }
         }
-        if (g.tokens_wg) break;
     }
 }
 

@@ -100,14 +100,29 @@ def test_refusals_of_the_c_interface(comet):
         assert rope(**bad) == comet.ERR_INVALID, bad
 
 
-def test_work_bytes_cover_every_piece(comet):
+def test_work_bytes(comet):
+    """Room for the pieces of tiles that are cut, whose number does not grow with the sequences, and 8 bytes per tile."""
     L = comet.lib()
-    for heads, group, seqs, tokens, dim in [(1, 1, 1, 1, 32), (8, 4, 64, 64, 128), (3, 40, 5, 1000, 256)]:
-        shape = comet.CacheShape(4, 64, 2, heads, dim)
-        tiles = tokens * group // 32 + seqs
-        assert L.comet_cache_attend_work(shape, seqs, tokens, heads * group) >= (-(-1 // heads) + tiles) * heads * 32 * (dim + 3) * 4
-    assert L.comet_cache_attend_work(comet.CacheShape(4, 64, 2, 8, 128), 1, 1, 12) == 0
-    assert L.comet_cache_attend_work(comet.CacheShape(4, 64, 2, 1, 128), 1, 1 << 30, 16) == 0
+    few = comet.CacheShape(4, 64, 2, 8, 128)
+    small, large = L.comet_cache_attend_work(few, 64, 64, 32), L.comet_cache_attend_work(few, 4096, 4096, 32)
+    assert 768 * 16 * (128 + 3) * 4 <= small < 64 << 20 and large - small < 16 * 4096 * 4
+    assert L.comet_cache_attend_work(few, 1, 8192, 32) >= 512 * 128 * (128 + 3) * 4
+    for bad in [(few, 1, 1, 12), (few, 1, 1, 0), (few, (1 << 22) + 1, 1, 32), (comet.CacheShape(4, 64, 2, 1, 128), 1, 1 << 30, 16),
+                (comet.CacheShape(4, 64, 2, 4096, 128), 8192, 8192, 4096)]:
+        assert L.comet_cache_attend_work(*bad) == 0, bad
+
+
+def test_results_must_not_overlap(comet):
+    """Tensors that are written: rows closer to each other than they are long are refused, in either direction; those that are read may be."""
+    L, shape, batch = comet.lib(), comet.CacheShape(4, 64, 2, 2, 64), C.byref(_batch(comet))
+    rows, plan = comet.CacheRows(FAKE, 128, 64), comet.RopePlan(64, 0, 1.0, FAKE)
+    for token, head in [(0, 64), (128, 0), (63, 64), (128, -63), (-1, 64)]:
+        bad = comet.CacheRows(FAKE + 4096, token, head)
+        assert L.comet_rope(C.byref(plan), rows, bad, 3, 2, 64, comet.F32, None, 0, None) == comet.ERR_INVALID
+        assert L.comet_cache_fetch(FAKE, shape, batch, 3, bad, rows, comet.F16, None, None) == comet.ERR_INVALID
+        assert L.comet_cache_fetch(FAKE, shape, batch, 3, rows, bad, comet.F16, None, None) == comet.ERR_INVALID
+        assert L.comet_cache_append(FAKE, shape, batch, 3, rows, rows, rows, bad, 4, comet.F16, None, None, None, None) == comet.ERR_INVALID
+        assert L.comet_cache_attend(FAKE, shape, batch, 3, rows, 4, comet.F16, 0.1, 1, bad, None, FAKE, 1 << 40, None, None) == comet.ERR_INVALID
 
 
 def test_binding_refuses_host_tensors(comet):

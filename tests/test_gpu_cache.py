@@ -378,6 +378,28 @@ def test_attend_short(comet, lens, new, causal):
     assert s.ok()
 
 
+@pytest.mark.parametrize("seqs,most_new,group", [(65, 1, 2), (300, 1, 4), (1000, 2, 1), (300, 40, 4), (40, 90, 2)])
+def test_many_sequences(comet, seqs, most_new, group):
+    """More sequences than a wavefront has lanes and than a workgroup has threads, some without tokens."""
+    g = gen(seqs)
+    s = Sequences(comet, torch.bfloat16, 1, 32, seqs, 320, seed=seqs)
+    s.grow(torch.randint(0, 200, (seqs,), generator=g).tolist())
+    new = torch.randint(0, most_new + 1, (seqs,), generator=g).tolist()
+    new[0], new[-1] = 0, most_new
+    s.grow(new)
+    q = s.tokens(sum(new), group)
+    out, lse = s.cache.comet_cache_attend(s.batch(new), q.cuda(), lse=True, status=s.status)
+    check_attend(s, new, q, out, lse)
+    k, v = s.cache.comet_cache_fetch(s.batch(new), dtype=s.dt, tokens=sum(new))
+    at = 0
+    for b, n in enumerate(new):
+        check_held(s, b)
+        want = s.held(b)[1][:, s.lens[b] - n:].transpose(0, 1)
+        assert ((v[at:at + n].cpu().double() - want).abs() <= (u(s.dt) + 2 * U32) * want.abs() + 2.0 ** -25).all()
+        at += n
+    assert s.ok()
+
+
 def test_attend_strides_and_options(comet):
     s = Sequences(comet, torch.float16, 2, 96, 2, 200, seed=2)
     s.grow([100, 50])

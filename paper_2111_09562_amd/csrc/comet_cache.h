@@ -113,6 +113,7 @@ __global__ void k_attend_join_tile(AttendArgs a);
 // ---- types ------------------------------------------------------------------------------------------------------
 using half8 = _Float16 __attribute__((ext_vector_type(8)));
 using half4 = _Float16 __attribute__((ext_vector_type(4)));
+using ushort2v = uint16_t __attribute__((ext_vector_type(2)));
 using half2v = _Float16 __attribute__((ext_vector_type(2)));
 using f32x16 = float __attribute__((ext_vector_type(16)));
 using f32x4 = float __attribute__((ext_vector_type(4)));

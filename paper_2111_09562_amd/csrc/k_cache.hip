@@ -78,12 +78,15 @@ __device__ inline float token_scale(float amax) {
 
 __device__ inline uint32_t larger16(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// A block's scale from the bits of its largest |value|, and a value in it.  A block with Inf or NaN has the scale NaN.
+// A block's scale from the bits of its largest |value|, and its values in whole numbers: added to 1.5 * 2^23 a product of at most 127 is rounded to the
+// nearest whole number (ties to even), whose low byte is the result's.  A block with Inf or NaN has the scale NaN and zeros (0 times
+// either is a NaN whose low byte is 0: a 16-bit NaN has none of its bits there).
 struct BlockScale {
     float scale, inv;
-    __device__ uint32_t to8(float x) const {
-        const float y = __builtin_rintf(x * inv);
-        return inv == 0.0f ? 0u : (uint32_t)(int32_t)__builtin_amdgcn_fmed3f(y, -127.0f, 127.0f) & 0xffu;
+    __device__ uint32_t bits(float x) const { return __float_as_uint(__builtin_fmaf(x, inv, 12582912.0f)); }
+    __device__ uint32_t pack(float x0, float x1, float x2, float x3) const {
+        const uint32_t lo = __builtin_amdgcn_perm(bits(x1), bits(x0), 0x0c0c0400u), hi = __builtin_amdgcn_perm(bits(x3), bits(x2), 0x04000c0cu);
+        return lo | hi;
     }
 };
 template <typename T>
@@ -95,24 +98,27 @@ __device__ inline BlockScale block_scale(uint32_t bits) {
     return s;
 }
 
+// Larger of two pairs of 16-bit numbers, each for itself.
+__device__ inline uint32_t larger16x2(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
+}
+
 // A block all of whose tokens are new, from the tensors to the cache in registers.  A thread has 16 keys of one token (a chunk of eight pairs, or 16
 // values that are not turned) and eight values of four tokens in a row, whose four bytes of a value lie side by side
 // in the cache: a token's eight threads write 32 bytes each of up to 8 kilobytes, eight threads the 32 bytes of a value.
 template <typename T>
 __device__ void compress_block(const AppendArgs &a, const Seq &s, uint32_t before, uint32_t seq, uint32_t head, uint32_t j) {
-    __shared__ uint32_t s_top[2][kCacheBlock / kWave];
+    __shared__ uint32_t s_top[kCacheBlock / kWave];
     constexpr int kMost = kCacheMaxDim / 128;              // items of a thread, at most
     const uint32_t tid = threadIdx.x, dim = a.c.dim, per_row = dim / 16u;
     const uint32_t rot = a.rope.steps ? a.rope.rot : 0u, rot_chunks = rot / 16u;
-    const int64_t index = block_index(a.b, a.c, seq, head, j);
-    if (index < 0) return;
     const int32_t token0 = s.start + (int32_t)(j * kBlk - before);
     typename Vec<T, 8>::type ka[kMost], kb[kMost], v[kMost / 2][4];
     uint32_t mk = 0, mv = 0;
     const auto top_of = [](const typename Vec<T, 8>::type &x, uint32_t m) {
         const u32x4 w = __builtin_bit_cast(u32x4, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m = larger16(m, larger16(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+        for (int i = 0; i < 4; ++i) m = larger16x2(m, w[i] & 0x7fff7fffu);
         return m;
     };
     const auto first_of = [&](uint32_t c) { return c < rot_chunks ? chunk_at<8>(a.rope, c) : rot + 16u * (c - rot_chunks); };
@@ -135,6 +141,7 @@ __device__ void compress_block(const AppendArgs &a, const Seq &s, uint32_t befor
             for (int u = 0; u < 4; ++u) v[n][u] = *reinterpret_cast<const typename Vec<T, 8>::type *>(p + u * a.v.token);
         }
     }
+    const int64_t index = block_index(a.b, a.c, seq, head, j);           // (asked for behind the rows, waited for with them)
 #pragma unroll
     for (int n = 0; n < kMost; ++n) {
         const uint32_t i = tid + n * kCacheBlock, row = i / per_row, c = i - row * per_row;
@@ -157,30 +164,26 @@ __device__ void compress_block(const AppendArgs &a, const Seq &s, uint32_t befor
 #pragma unroll
             for (int u = 0; u < 4; ++u) mv = top_of(v[n][u], mv);
         }
+    uint32_t both = larger16(mk & 0xffffu, mk >> 16) | larger16(mv & 0xffffu, mv >> 16) << 16;
 #pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        mk = larger16(mk, (uint32_t)__shfl_xor((int)mk, o, kWave));
-        mv = larger16(mv, (uint32_t)__shfl_xor((int)mv, o, kWave));
-    }
-    if (lane_id() == 0) { s_top[0][tid / kWave] = mk; s_top[1][tid / kWave] = mv; }
+    for (int o = 1; o < kWave; o <<= 1) both = larger16x2(both, (uint32_t)__shfl_xor((int)both, o, kWave));
+    if (lane_id() == 0) s_top[tid / kWave] = both;
     __syncthreads();
 #pragma unroll
-    for (uint32_t w = 0; w < kCacheBlock / kWave; ++w) { mk = larger16(mk, s_top[0][w]); mv = larger16(mv, s_top[1][w]); }
-    const BlockScale sk = block_scale<T>(mk), sv = block_scale<T>(mv);
+    for (uint32_t w = 0; w < kCacheBlock / kWave; ++w) both = larger16x2(both, s_top[w]);
+    if (index < 0) return;
+    const BlockScale sk = block_scale<T>(both & 0xffffu), sv = block_scale<T>(both >> 16);
     uint8_t *to = a.c.blocks + (uint64_t)index * 64u * dim;
 #pragma unroll
     for (int n = 0; n < kMost; ++n) {
         const uint32_t i = tid + n * kCacheBlock, row = i / per_row, c = i - row * per_row;
         if (row < (uint32_t)kBlk) {
             const uint32_t d = first_of(c), e = d + second_of(c);
-            uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                w[u / 4] |= sk.to8((float)ka[n][u]) << (8 * (u % 4));
-                w[2 + u / 4] |= sk.to8((float)kb[n][u]) << (8 * (u % 4));
-            }
-            *reinterpret_cast<uint2 *>(to + d / 32u * 1024u + row * 32u + d % 32u) = uint2{w[0], w[1]};
-            *reinterpret_cast<uint2 *>(to + e / 32u * 1024u + row * 32u + e % 32u) = uint2{w[2], w[3]};
+            const auto quant = [&](const typename Vec<T, 8>::type &x) {
+                return uint2{sk.pack((float)x[0], (float)x[1], (float)x[2], (float)x[3]), sk.pack((float)x[4], (float)x[5], (float)x[6], (float)x[7])};
+            };
+            *reinterpret_cast<uint2 *>(to + d / 32u * 1024u + row * 32u + d % 32u) = quant(ka[n]);
+            *reinterpret_cast<uint2 *>(to + e / 32u * 1024u + row * 32u + e % 32u) = quant(kb[n]);
         }
     }
 #pragma unroll
@@ -189,12 +192,8 @@ __device__ void compress_block(const AppendArgs &a, const Seq &s, uint32_t befor
         if (d < dim) {
             uint8_t *at = to + 32u * dim + 32u * d + place_of(4u * quad);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                uint32_t w = 0u;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) w |= sv.to8((float)v[n][u][k]) << (8 * u);
-                *reinterpret_cast<uint32_t *>(at + 32u * k) = w;
-            }
+            for (int k = 0; k < 8; ++k)
+                *reinterpret_cast<uint32_t *>(at + 32u * k) = sv.pack((float)v[n][0][k], (float)v[n][1][k], (float)v[n][2][k], (float)v[n][3][k]);
         }
     }
     if (tid < 2u) a.c.scales[2u * (uint64_t)index + tid] = tid ? sv.scale : sk.scale;
@@ -314,17 +313,20 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
                 const BlockScale scale[2] = {block_scale<T>(m[0]), block_scale<T>(m[1])};
                 uint8_t *to = a.c.blocks + (uint64_t)index * 64u * dim;
                 for (uint32_t i = tid; i < 4u * dim; i += kCacheBlock) {       // 16 bytes each: keys, then values
-                    uint32_t w[4] = {0u, 0u, 0u, 0u};
+                    uint32_t w[4];
+                    float x[16];
                     if (i < 2u * dim) {
                         const uint32_t c = i / 64u, row = (i / 2u) % 32u, h = i % 2u;
-                        const uint16_t *p = kt + row * pitch + c * 32u + h * 16u;
-#pragma unroll
-                        for (int u = 0; u < 16; ++u) w[u / 4] |= scale[0].to8(widen<T>(p[u])) << (8 * (u % 4));
+                        load_row<T, 8>(x, reinterpret_cast<const T *>(kt + row * pitch + c * 32u + h * 16u));
+                        load_row<T, 8>(x + 8, reinterpret_cast<const T *>(kt + row * pitch + c * 32u + h * 16u + 8u));
                     } else {
                         const uint32_t d = (i - 2u * dim) / 2u, h = i % 2u;
 #pragma unroll
-                        for (int u = 0; u < 16; ++u) w[u / 4] |= scale[1].to8(widen<T>(vt[token_at(16u * h + u) * pitch + d])) << (8 * (u % 4));
+                        for (int u = 0; u < 16; ++u) x[u] = widen<T>(vt[token_at(16u * h + u) * pitch + d]);
                     }
+                    const BlockScale of = i < 2u * dim ? scale[0] : scale[1];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) w[u] = of.pack(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
                     *reinterpret_cast<u32x4 *>(to + 16u * i) = u32x4{w[0], w[1], w[2], w[3]};
                 }
                 if (tid < 2u) a.c.scales[2u * (uint64_t)index + tid] = tid ? scale[1].scale : scale[0].scale;

@@ -105,6 +105,8 @@ template <int NC>
 __global__ void k_attend(AttendArgs a);
 template <int NC, bool EXACT>
 __global__ void k_attend_few(AttendArgs a);
+// Where the registers are enough for two wavefronts per SIMD, those fill each other's gaps; a single one's instructions are interleaved by hand.
+constexpr bool tile_pairs(int nc, int rt) { return nc * rt <= 4; }
 template <int NC, int RT>
 __global__ void k_attend_tile(AttendArgs a);
 __global__ void k_attend_join(AttendArgs a);

@@ -95,9 +95,9 @@ void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tok
 
 // Workgroups an attention call is cut into, about.  Few rows: 768 are resident at once for heads of 128; many sequences of different lengths
 // (64 x 400 .. 16384 tokens, 8 heads) take 122 us with 768, 127 with 512, two long ones (120000 tokens, 8 heads) 104 with 768, 99 with 512.
-// Many rows: beyond 512 pieces what they leave for the join costs more than shorter pieces save (prompts of 500 to 2000 tokens, 8 heads: 117 us
-// with 512, 153 with 768).
-constexpr uint32_t kAttendPieces = 768, kAttendPiecesLong = 512, kAttendTilePieces = 512;
+// Many rows: as many as are resident, one or two per compute unit.  Beyond that what they leave for the join costs more than shorter pieces save
+// (prompts of 500 to 2000 tokens, 8 heads: 117 us with 512, 153 with 768).
+constexpr uint32_t kAttendPieces = 768, kAttendPiecesLong = 512, kAttendTilePieces = 256;
 struct AttendPlan {
     uint32_t pieces, grid, slots, tiles, tile_shift, min_blocks;
     bool few, wide, two;                                 // k_attend_few; k_attend_tile; that with two tiles of 32 rows per wavefront
@@ -114,7 +114,9 @@ bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32
     p->few = rows <= 16ull * n_seqs;
     p->tile_shift = p->few ? 4u : !p->wide ? 5u : p->two ? 8u : 7u;
     p->tiles = (uint32_t)(rows >> p->tile_shift) + n_seqs;
-    p->pieces = ((p->wide ? kAttendTilePieces : (uint64_t)p->tiles * s.heads < 128u ? kAttendPiecesLong : kAttendPieces) + s.heads - 1u) / s.heads;
+    const uint32_t pieces = !p->wide ? ((uint64_t)p->tiles * s.heads < 128u ? kAttendPiecesLong : kAttendPieces)
+                                     : kAttendTilePieces * (tile_pairs((int)s.dim / 32, p->two ? 2 : 1) ? 2u : 1u);
+    p->pieces = (pieces + s.heads - 1u) / s.heads;
     p->min_blocks = p->wide ? 16u : 4u;
     // A tile's pieces are counted as if it saw all of its sequence: of tiles of a causal prompt up to half have nothing to do.  Tiles that are cut
     // have more than total / pieces blocks, so there are at most `pieces` of them (twice that), each with one piece more than its share.
@@ -288,14 +290,12 @@ int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const com
         default: launch_attend<8>(a, p, wg, st); break;
     }
     HIP_TRY(hipGetLastError());
-    const uint32_t groups = p.tiles * shape.heads;
-    if (p.wide) {
-        k_attend_join_tile<<<dim3(groups, 8u), kAttendBlock, 0, st>>>(a);
-    } else {
-        uint32_t side = 4096u / groups;                 // the rows of a tile side by side while there are few tiles
-        side = side < 1u ? 1u : (side > a.tile_rows ? a.tile_rows : side);
-        k_attend_join<<<dim3(groups, side), kAttendBlock, 0, st>>>(a);
-    }
+    // the rows of a tile side by side while there are few tiles
+    const uint32_t groups = p.tiles * shape.heads, most = p.wide ? 8u : a.tile_rows;
+    uint32_t side = (p.wide ? 2048u : 4096u) / groups;
+    side = side < 1u ? 1u : (side > most ? most : side);
+    if (p.wide) k_attend_join_tile<<<dim3(groups, side), kAttendBlock, 0, st>>>(a);
+    else k_attend_join<<<dim3(groups, side), kAttendBlock, 0, st>>>(a);
     HIP_TRY(hipGetLastError());
     return COMET_OK;
 }

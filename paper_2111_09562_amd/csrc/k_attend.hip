@@ -367,14 +367,15 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_join(AttendArgs a) {
     __shared__ __align__(16) float s_o[kAttendBlock][4];
     const uint32_t tid = threadIdx.x, lane = (uint32_t)lane_id(), dim = a.c.dim;
     const uint32_t unit = blockIdx.x / a.c.heads, head = blockIdx.x - unit * a.c.heads;
+    // (units that no tile has are unwritten: whatever they hold, what follows finds out)
+    const uint32_t slot0 = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
+    if (parts < 2u || slot0 >= a.slots || parts > a.slots - slot0) return;
     const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, a.group, a.tile_shift, 1u);
     const uint32_t first = first_unit(a.b.starts, seq, a.group, a.tile_shift, 1u);
     SeqWork w;
     w.read(a, seq);
     const uint32_t tile = unit - first, tiles = w.tiles;
     if (unit < first || tile >= tiles) return;
-    const uint32_t slot0 = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
-    if (parts < 2u || slot0 >= a.slots || parts > a.slots - slot0) return;   // (starts that make no sense leave entries unwritten)
     const uint32_t rows = (uint32_t)w.s.n * a.group;
     const uint32_t quads = dim / 4u, lots = kAttendBlock / quads, lot = tid / quads, quad = tid - lot * quads;    // lots: pieces at a time
     for (uint32_t n = blockIdx.y; n < a.tile_rows && tile * a.tile_rows + n < rows; n += gridDim.y) {
@@ -418,14 +419,15 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_join(AttendArgs a) {
 __global__ __launch_bounds__(kAttendBlock) void k_attend_join_tile(AttendArgs a) {
     const uint32_t lane = (uint32_t)lane_id(), dim = a.c.dim;
     const uint32_t unit = blockIdx.x / a.c.heads, head = blockIdx.x - unit * a.c.heads;
+    // (units that no tile has are unwritten: whatever they hold, what follows finds out)
+    const uint32_t slot0 = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
+    if (parts < 2u || slot0 >= a.slots || parts > a.slots - slot0) return;
     const uint32_t seq = find_sequence(a.b.starts, a.b.n_seqs, unit, a.group, a.tile_shift, 1u);
     const uint32_t first = first_unit(a.b.starts, seq, a.group, a.tile_shift, 1u);
     SeqWork w;
     w.read(a, seq);
     const uint32_t tile = unit - first, tiles = w.tiles;
     if (unit < first || tile >= tiles) return;
-    const uint32_t slot0 = (uint32_t)a.directory[2u * unit], parts = (uint32_t)a.directory[2u * unit + 1u];
-    if (parts < 2u || slot0 >= a.slots || parts > a.slots - slot0) return;
     const uint32_t rows = (uint32_t)w.s.n * a.group;
     for (uint32_t n = blockIdx.y * 4u + threadIdx.x / kWave; n < a.tile_rows && tile * a.tile_rows + n < rows; n += 4u * gridDim.y) {
         const uint32_t row = tile * a.tile_rows + n, query = row / a.group, qh = head * a.group + (row - query * a.group);

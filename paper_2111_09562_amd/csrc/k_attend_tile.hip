@@ -15,8 +15,6 @@ __device__ inline void interleave(half8 *p, float &l) {
         __builtin_amdgcn_sched_group_barrier(0x402, PER, 0);             // vector instructions
     }
 }
-// Where the registers are enough for two wavefronts per SIMD, those fill each other's gaps; a single one's instructions are interleaved by hand.
-constexpr bool tile_pairs(int nc, int rt) { return nc * rt <= 4; }
 }  // namespace
 
 // Many rows: the four wavefronts of a workgroup hold 32 * RT rows each and go through the same blocks together.  Every block is converted to

@@ -168,5 +168,6 @@ def _turn(x, rope, positions, backward):
 
 def rotate(x, rope: "comet.Rope", positions=None):
     """x [tokens, heads, dim] turned by its tokens' positions (``comet.comet_rope``), differentiable.  The gradient is the rotation the other
-    way, so nothing but ``positions`` is kept for the backward pass."""
+    way, so nothing but ``positions`` is kept for the backward pass.  As for every operation: a backward pass that is captured into a graph must
+    not share leaves with one outside that is still alive."""
     return _Rotate.apply(x, rope, positions, False)

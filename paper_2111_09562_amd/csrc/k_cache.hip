@@ -1,4 +1,6 @@
-// Keys and values into the compressed cache and out of it again.  Bound by HBM for prompts, by latency for single tokens.
+// Keys and values into the compressed cache and out of it again.  Bound by HBM for prompts, by a chain of memory round trips for single tokens.
+// 18792 tokens, 8 + 8 heads of 128, bf16: in 39 us (3.0 TB/s; 31 without the rotation), with 32 heads of queries 103 us (4.1 TB/s), out 21 us
+// (5.6 TB/s).  64 single tokens: in 7.6 us, 12.7 if all of them complete a block, out 3.5.
 #include "comet_cache.h"
 
 namespace comet {

@@ -111,6 +111,47 @@ def test_rope_gradient(comet):
     assert torch.isfinite(xd.grad).all()
 
 
+def test_rope_second_gradient_and_capture(comet):
+    """Positions 0, 1, ..; the gradient of the gradient (a rotation again); a training step captured in a graph follows its inputs."""
+    from paper_2111_09562_amd import autograd
+    rope = comet.Rope(64)
+    g = gen(11)
+    x, w, z = (torch.randn(40, 3, 64, generator=g, device="cpu") for _ in range(3))
+    xd, wd = x.cuda().requires_grad_(), w.cuda().requires_grad_()
+    (dx,) = torch.autograd.grad(autograd.rotate(xd, rope), xd, wd, create_graph=True)
+    (dw,) = torch.autograd.grad(dx, wd, z.cuda())
+    positions = torch.arange(40)
+    y, tol = rope_bound(w, positions, 64, False, {}, -1.0)
+    assert ((dx.detach().cpu().double() - y).abs() <= tol).all()
+    y, tol = rope_bound(z, positions, 64, False, {})
+    assert ((dw.cpu().double() - y).abs() <= tol).all()
+
+    pos = torch.zeros(40, dtype=torch.int32, device="cuda")
+    static, grad = torch.zeros(40, 3, 64, device="cuda"), torch.zeros(40, 3, 64, device="cuda")
+
+    def step():
+        leaf = static.detach().requires_grad_()
+        out = autograd.rotate(leaf, rope, pos)
+        return out.detach(), torch.autograd.grad(out, leaf, grad)[0]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, dleaf = step()
+    for i in range(5):
+        static.copy_(torch.randn(static.shape, generator=g))
+        grad.copy_(torch.randn(static.shape, generator=g))
+        pos.copy_(torch.randint(0, 1 << 16, (40,), generator=g, dtype=torch.int32))
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(dleaf, want[1])
+
+
 # ---- sequences in a cache -----------------------------------------------------------------------------------------
 
 

@@ -93,11 +93,14 @@ void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tok
     k_rope<T, V><<<wg, kRopeBlock, 0, st>>>(r, g, x, y, n_tokens, heads, dim, sign);
 }
 
-// Workgroups an attention call is cut into, about.  Few rows: 768 are resident at once for heads of 128; many sequences of different lengths
-// (64 x 400 .. 16384 tokens, 8 heads) take 122 us with 768, 127 with 512, two long ones (120000 tokens, 8 heads) 104 with 768, 99 with 512.
+// Workgroups an attention call is cut into, about.  Few rows: 768 are resident at once for heads of 128; more than that even out sequences of
+// different lengths (64 x 400 .. 16384 tokens, 8 heads: 119 us with 768, 114 with 1280, 117 with 1536), as long as a piece keeps the keys and
+// values of 32 x 2048 / dim tokens, 128 KB: beneath that, writing and joining its result costs more (16 x 4096 tokens, 8 heads of 256: 33 us,
+// with half of that 39; with heads of 64 29 and 33; 16 x 2000 .. 4000 tokens of 5 queries 27 either way, 25 with 768).  Where there are few
+// tiles, two long sequences say (120000 tokens, 8 heads), 512 pieces take 99 us, 768 take 104.
 // Many rows: as many as are resident, one or two per compute unit.  Beyond that what they leave for the join costs more than shorter pieces save
 // (prompts of 500 to 2000 tokens, 8 heads: 117 us with 512, 153 with 768).
-constexpr uint32_t kAttendPieces = 768, kAttendPiecesLong = 512, kAttendTilePieces = 256;
+constexpr uint32_t kAttendPieces = 1280, kAttendPiecesLong = 512, kAttendTilePieces = 256;
 struct AttendPlan {
     uint32_t pieces, grid, slots, tiles, tile_shift, min_blocks;
     bool few, wide, two;                                 // k_attend_few; k_attend_tile; that with two tiles of 32 rows per wavefront
@@ -114,10 +117,11 @@ bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32
     p->few = rows <= 16ull * n_seqs;
     p->tile_shift = p->few ? 4u : !p->wide ? 5u : p->two ? 8u : 7u;
     p->tiles = (uint32_t)(rows >> p->tile_shift) + n_seqs;
-    const uint32_t pieces = !p->wide ? ((uint64_t)p->tiles * s.heads < 128u ? kAttendPiecesLong : kAttendPieces)
+    const bool lone = (uint64_t)p->tiles * s.heads < 128u;
+    const uint32_t pieces = !p->wide ? (lone ? kAttendPiecesLong : kAttendPieces)
                                      : kAttendTilePieces * (tile_pairs((int)s.dim / 32, p->two ? 2 : 1) ? 2u : 1u);
     p->pieces = (pieces + s.heads - 1u) / s.heads;
-    p->min_blocks = p->wide ? 16u : 4u;
+    p->min_blocks = p->wide ? 16u : lone ? 4u : 2048u / s.dim;
     // A tile's pieces are counted as if it saw all of its sequence: of tiles of a causal prompt up to half have nothing to do.  Tiles that are cut
     // have more than total / pieces blocks, so there are at most `pieces` of them (twice that), each with one piece more than its share.
     const uint64_t most = (p->wide ? 2u : 1u) * (uint64_t)p->pieces, grid = (most + p->tiles) * s.heads, n = (uint64_t)(2u * most) * s.heads, per = 1ull << p->tile_shift;

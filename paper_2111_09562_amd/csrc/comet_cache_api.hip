@@ -95,9 +95,10 @@ void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tok
 
 // Workgroups an attention call is cut into, about.  Few rows: 768 are resident at once for heads of 128; more than that even out sequences of
 // different lengths (64 x 400 .. 16384 tokens, 8 heads: 119 us with 768, 114 with 1280, 117 with 1536), as long as a piece keeps the keys and
-// values of 32 x 2048 / dim tokens, 128 KB: beneath that, writing and joining its result costs more (16 x 4096 tokens, 8 heads of 256: 33 us,
-// with half of that 39; with heads of 64 29 and 33; 16 x 2000 .. 4000 tokens of 5 queries 27 either way, 25 with 768).  Where there are few
-// tiles, two long sequences say (120000 tokens, 8 heads), 512 pieces take 99 us, 768 take 104.
+// values of 2048 / dim blocks, 128 KB: beneath that, writing and joining its result costs more (64 x 300 .. 4000 tokens, 2 heads of 256: 33 us,
+// with pieces half as long 39; 128 x 500 .. 3000 tokens, 4 heads of 64: 29 and 33).  Short sequences gain nothing (48 x 8 .. 4096 tokens, 12
+// heads of 64: 25 us with 768, 27 with 1280).  Where there are few tiles, two long sequences say (120000 tokens, 8 heads), 512 pieces take 99 us,
+// 768 take 104.
 // Many rows: as many as are resident, one or two per compute unit.  Beyond that what they leave for the join costs more than shorter pieces save
 // (prompts of 500 to 2000 tokens, 8 heads: 117 us with 512, 153 with 768).
 constexpr uint32_t kAttendPieces = 1280, kAttendPiecesLong = 512, kAttendTilePieces = 256;

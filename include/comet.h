@@ -231,7 +231,8 @@ int comet_controller_update(comet_controller *c, const float *eb_old, const floa
  * touch is skipped: rows left as they were, tokens of a page that is none not seen.  A token whose key (value) holds Inf or NaN makes NaN of
  * the keys (values) of its block and head when read back, and of the rows that see any of the block.
  *
- * Tensors are [tokens][heads][dim] with strides in elements; the dim values of a row are contiguous.  dtype: COMET_F16 or COMET_BF16
+ * Tensors are [tokens][heads][dim] with strides in elements; the dim values of a row are contiguous; in those that are written no two rows may overlap,
+ * and the rows of a token lie between those of its neighbours, or the rows of a head (else COMET_ERR_INVALID).  dtype: COMET_F16 or COMET_BF16
  * (comet_rope: COMET_F32 too).  Everything is asynchronous on `stream` and may be captured into a HIP graph; a replay
  * goes by what the batch's arrays hold then.  Nothing is allocated. */
 #define COMET_F32 0
@@ -281,7 +282,7 @@ int comet_cache_fetch(const void *dev_cache, comet_cache_shape shape, const come
 /* Attention of the batch's queries over the cache: out = softmax(scale * q k^T) v, query heads h * q_heads/heads .. sharing key/value head h.
  * causal != 0: a query sees the tokens up to its own place (n queries are the last n of lens[b] tokens; those in front of
  * the first see nothing); 0: all lens[b].  A row that sees nothing is 0 and its lse -Inf.  dev_lse: float32[n_tokens][q_heads],
- * log of the sum of exp of the row's scores, or NULL.  scale: finite, >= 0.  dev_work: comet_cache_attend_work bytes, 16-byte aligned, whose contents
+ * log of the sum of exp of the row's scores, or NULL.  out must not overlap q.  scale: finite, >= 0.  dev_work: comet_cache_attend_work bytes, 16-byte aligned, whose contents
  * need no initialisation; calls that can overlap in time need one each. */
 uint64_t comet_cache_attend_work(comet_cache_shape shape, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads);
 int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const comet_cache_batch *batch, uint32_t n_tokens, comet_rows q, uint32_t q_heads,

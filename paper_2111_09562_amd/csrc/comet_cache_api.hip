@@ -57,10 +57,13 @@ bool rows_args(comet_rows r, int dtype, Rows *to) {
     to->p = static_cast<uint8_t *>(r.dev); to->token = r.token_stride; to->head = r.head_stride;
     return true;
 }
-// Rows that are written: no two of them may overlap.
+// Rows that are written: no two of them may overlap.  So the rows of a token lie between those of two tokens, or the rows of a head between
+// those of two heads.
 bool out_args(comet_rows r, int dtype, uint32_t tokens, uint32_t heads, uint32_t dim, Rows *to) {
-    const auto apart = [dim](int64_t stride) { return stride >= (int64_t)dim || stride <= -(int64_t)dim; };
-    return rows_args(r, dtype, to) && (tokens < 2u || apart(r.token_stride)) && (heads < 2u || apart(r.head_stride));
+    const auto size = [](int64_t stride) { return stride < 0 ? 0 - (unsigned __int128)(__int128)stride : (unsigned __int128)stride; };
+    const unsigned __int128 token = tokens < 2u ? 0 : size(r.token_stride), head = heads < 2u ? 0 : size(r.head_stride);
+    const bool tokens_apart = tokens < 2u || token >= head * (heads - 1u) + dim, heads_apart = heads < 2u || head >= token * (tokens - 1u) + dim;
+    return rows_args(r, dtype, to) && (tokens < 2u || token >= dim) && (heads < 2u || head >= dim) && (tokens_apart || heads_apart);
 }
 bool rows_aligned(const Rows &r, int dtype) {                                   // every row begins at a multiple of 16 bytes
     const int64_t v = 16 / elem_size(dtype);
@@ -272,7 +275,8 @@ int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const com
         !std::isfinite(scale * 1.4426950408889634f) || scale < 0.0f || (uintptr_t)dev_lse % 4u || !plan_attend(shape, batch->n_seqs, n_tokens, q_heads, &p))
         return COMET_ERR_INVALID;
     if (!n_tokens) return COMET_OK;
-    if (!rows_args(q, dtype, &a.q) || !out_args(out, dtype, n_tokens, q_heads, shape.dim, &a.out) || !dev_work || (uintptr_t)dev_work % 16u) return COMET_ERR_INVALID;
+    if (!rows_args(q, dtype, &a.q) || !out_args(out, dtype, n_tokens, q_heads, shape.dim, &a.out) || q.dev == out.dev || !dev_work || (uintptr_t)dev_work % 16u)
+        return COMET_ERR_INVALID;
     if (work_bytes < p.bytes) return COMET_ERR_NOMEM;
     a.lse = dev_lse; a.q_heads = q_heads; a.group = q_heads / shape.heads;
     a.bf16 = dtype == COMET_BF16; a.causal = causal != 0; a.wide = p.wide; a.vec = rows_aligned(a.q, dtype) && rows_aligned(a.out, dtype);

@@ -60,12 +60,13 @@ def _batch(comet, **over):
 def test_refusals_of_the_c_interface(comet):
     L = comet.lib()
     ok_shape, rows = comet.CacheShape(4, 64, 2, 2, 64), comet.CacheRows(FAKE, 128, 64)
+    queries, results = comet.CacheRows(FAKE, 256, 64), comet.CacheRows(FAKE + 4096, 256, 64)
     plan = comet.RopePlan(64, 0, 1.0, FAKE)
 
-    def append(cache=FAKE, shape=ok_shape, batch=None, n=3, k=rows, v=rows, q=rows, qo=rows, qh=4, dt=comet.F16, p=plan, pos=FAKE, status=None):
+    def append(cache=FAKE, shape=ok_shape, batch=None, n=3, k=rows, v=rows, q=queries, qo=queries, qh=4, dt=comet.F16, p=plan, pos=FAKE, status=None):
         return L.comet_cache_append(cache, shape, C.byref(batch or _batch(comet)), n, k, v, q, qo, qh, dt, C.byref(p), pos, None, status)
 
-    def attend(cache=FAKE, shape=ok_shape, batch=None, n=3, q=rows, qh=4, dt=comet.F16, scale=0.1, out=rows, lse=None, work=FAKE, size=1 << 40):
+    def attend(cache=FAKE, shape=ok_shape, batch=None, n=3, q=queries, qh=4, dt=comet.F16, scale=0.1, out=results, lse=None, work=FAKE, size=1 << 40):
         return L.comet_cache_attend(cache, shape, C.byref(batch or _batch(comet)), n, q, qh, dt, scale, 1, out, lse, work, size, None, None)
 
     def fetch(cache=FAKE, shape=ok_shape, batch=None, n=3, k=rows, v=rows, dt=comet.F16):
@@ -82,11 +83,11 @@ def test_refusals_of_the_c_interface(comet):
     for call in (append, fetch):
         for bad in [dict(k=none), dict(v=none), dict(k=odd), dict(v=odd)]:
             assert call(**bad) == comet.ERR_INVALID
-    for bad in [dict(q=none), dict(qo=odd), dict(qo=comet.CacheRows(FAKE, 256, 64)), dict(qh=20000), dict(p=comet.RopePlan(66, 0, 1.0, FAKE)),
+    for bad in [dict(q=none), dict(qo=odd), dict(qo=comet.CacheRows(FAKE, 512, 64)), dict(qh=20000), dict(p=comet.RopePlan(66, 0, 1.0, FAKE)),
                 dict(p=comet.RopePlan(64, 2, 1.0, FAKE)), dict(p=comet.RopePlan(64, 0, float("nan"), FAKE)), dict(p=comet.RopePlan(64, 0, 1.0, None)),
                 dict(p=comet.RopePlan(0, 0, 1.0, FAKE)), dict(pos=FAKE + 1), dict(status=FAKE + 3)]:
         assert append(**bad) == comet.ERR_INVALID, bad
-    for bad in [dict(q=none), dict(out=odd), dict(qh=0), dict(qh=3), dict(scale=float("nan")), dict(scale=-1.0), dict(scale=float("inf")), dict(lse=FAKE + 2),
+    for bad in [dict(q=none), dict(out=odd), dict(out=queries), dict(qh=0), dict(qh=3), dict(scale=float("nan")), dict(scale=-1.0), dict(scale=float("inf")), dict(lse=FAKE + 2),
                 dict(work=None), dict(work=FAKE + 4), dict(n=0x7fffffff)]:
         assert attend(**bad) == comet.ERR_INVALID, bad
     assert attend(size=L.comet_cache_attend_work(ok_shape, 2, 3, 4) - 1) == comet.ERR_NOMEM
@@ -123,6 +124,22 @@ def test_results_must_not_overlap(comet):
         assert L.comet_cache_fetch(FAKE, shape, batch, 3, rows, bad, comet.F16, None, None) == comet.ERR_INVALID
         assert L.comet_cache_append(FAKE, shape, batch, 3, rows, rows, rows, bad, 4, comet.F16, None, None, None, None) == comet.ERR_INVALID
         assert L.comet_cache_attend(FAKE, shape, batch, 3, rows, 4, comet.F16, 0.1, 1, bad, None, FAKE, 1 << 40, None, None) == comet.ERR_INVALID
+
+
+def test_results_must_not_interleave(comet):
+    """Rows that are apart from their neighbours can still lie on those of another token's other head; attention's result not on its queries."""
+    L, shape, batch = comet.lib(), comet.CacheShape(4, 64, 2, 2, 64), C.byref(_batch(comet))
+    rows, plan = comet.CacheRows(FAKE, 128, 64), comet.RopePlan(64, 0, 1.0, FAKE)
+    low = -(1 << 63)
+    for tokens, heads, token, head in [(2, 2, 64, 64), (3, 2, 128, 128), (3, 4, 191, 64), (2, 3, 64, 127), (3, 2, -128, 128), (3, 2, 64, 191), (3, 2, low, low)]:
+        bad = comet.CacheRows(FAKE + 4096, token, head)
+        assert L.comet_rope(C.byref(plan), rows, bad, tokens, heads, 64, comet.F32, None, 0, None) == comet.ERR_INVALID, (tokens, heads, token, head)
+    bad = comet.CacheRows(FAKE + 4096, 64, 64)
+    assert L.comet_cache_fetch(FAKE, shape, batch, 3, bad, rows, comet.F16, None, None) == comet.ERR_INVALID
+    assert L.comet_cache_append(FAKE, shape, batch, 3, rows, rows, rows, bad, 4, comet.F16, None, None, None, None) == comet.ERR_INVALID
+    assert L.comet_cache_attend(FAKE, shape, batch, 3, rows, 4, comet.F16, 0.1, 1, bad, None, FAKE, 1 << 40, None, None) == comet.ERR_INVALID
+    assert L.comet_cache_attend(FAKE, shape, batch, 3, comet.CacheRows(FAKE, 256, 64), 4, comet.F16, 0.1, 1, comet.CacheRows(FAKE, 256, 64), None, FAKE, 1 << 40,
+                                None, None) == comet.ERR_INVALID
 
 
 def test_binding_refuses_host_tensors(comet):

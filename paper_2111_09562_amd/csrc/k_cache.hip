@@ -1,6 +1,6 @@
 // Keys and values into the compressed cache and out of it again.  Bound by HBM for prompts, by a chain of memory round trips for single tokens.
 // 18792 tokens, 8 + 8 heads of 128, bf16: in 39 us (3.0 TB/s; 31 without the rotation), with 32 heads of queries 103 us (4.1 TB/s), out 21 us
-// (5.6 TB/s).  64 single tokens: in 7.6 us, 12.7 if all of them complete a block, out 3.5.
+// (5.6 TB/s).  64 single tokens: in 7.5 us, 11.5 if all of them complete a block, out 3.5.
 #include "comet_cache.h"
 
 namespace comet {
@@ -43,7 +43,7 @@ __device__ void load_block(const AppendArgs &a, const Seq &s, uint32_t before, u
             store_row<T, V>(reinterpret_cast<T *>(kt + row * pitch + at), x);
         }
     }
-    for (uint32_t i = threadIdx.x; i < (r1 - r0) * (dim / V); i += kCacheBlock) {
+    for (uint32_t i = threadIdx.x ^ 128u; i < (r1 - r0) * (dim / V); i += kCacheBlock) {      // (of few rows not by the wavefront that has the keys)
         const uint32_t row = r0 + i / (dim / V), d = i % (dim / V) * V, t = j * kBlk + row;
         const int32_t token = s.start + (int32_t)(t - before);
         float x[V];
@@ -54,19 +54,29 @@ __device__ void load_block(const AppendArgs &a, const Seq &s, uint32_t before, u
     const uint8_t *half = ring_half(a.c, slot, head, j);
     const uint16_t *kr = reinterpret_cast<const uint16_t *>(half), *vr = kr + 32u * dim;
     const float *e = reinterpret_cast<const float *>(half + 128ull * dim);
-    for (uint32_t i = threadIdx.x; i < r0 * (dim / 8u); i += kCacheBlock) {        // (r0 <= 31 tokens of before)
-        const uint32_t row = i / (dim / 8u), d = i % (dim / 8u) * 8u;
+    // A round's loads, eight values of a key and four tokens of two values, wait for memory together (larger rounds cost a wavefront per SIMD:
+    // 64 tokens that all complete a block 11.5 us, 10.9 with rounds twice that, 12.7 one load at a time; 18792 tokens 136, 143 and 136 with the fetch).
+    const uint32_t n_k = r0 * (dim / 8u), quad = token_at(4u * (threadIdx.x % 8u));           // (r0 <= 31 tokens of before)
+    const f32x4 ve = *reinterpret_cast<const f32x4 *>(e + 32u + quad);
+    for (uint32_t k0 = threadIdx.x, v0 = threadIdx.x; v0 < 8u * dim; k0 += kCacheBlock, v0 += 2u * kCacheBlock) {
+        const bool there = k0 < n_k;
+        const uint32_t row = there ? k0 / (dim / 8u) : 0u, d = there ? k0 % (dim / 8u) * 8u : 0u, v1 = v0 + kCacheBlock;
         const half8 k = *reinterpret_cast<const half8 *>(kr + (d / 32u * 32u + row) * 32u + d % 32u);
+        const float ke = e[row];
+        const half4 v[2] = {*reinterpret_cast<const half4 *>(vr + 4u * v0), *reinterpret_cast<const half4 *>(vr + 4u * (v1 < 8u * dim ? v1 : v0))};
+        if (there) {
 #pragma unroll
-        for (uint32_t u = 0; u < 8u; ++u) kt[row * pitch + d + u] = narrow<T>((float)k[u] * e[row]);
-    }
-    for (uint32_t i = threadIdx.x; i < 8u * dim; i += kCacheBlock) {               // four tokens of a value
-        const uint32_t d = i / 8u, row = token_at(4u * (i % 8u));
-        if (row >= r0) continue;
-        const half4 v = *reinterpret_cast<const half4 *>(vr + 4u * i);
+            for (uint32_t u = 0; u < 8u; ++u) kt[row * pitch + d + u] = narrow<T>((float)k[u] * ke);
+        }
 #pragma unroll
-        for (uint32_t u = 0; u < 4u; ++u)
-            if (row + u < r0) vt[(row + u) * pitch + d] = narrow<T>((float)v[u] * e[32u + row + u]);
+        for (uint32_t m = 0; m < 2u; ++m) {
+            const uint32_t at = m ? v1 : v0;
+            if (at < 8u * dim) {
+#pragma unroll
+                for (uint32_t u = 0; u < 4u; ++u)
+                    if (quad + u < r0) vt[(quad + u) * pitch + at / 8u] = narrow<T>((float)v[m][u] * ve[u]);
+            }
+        }
     }
 }
 
@@ -278,6 +288,7 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
         const uint32_t r0 = jj * kBlk < before ? before - jj * kBlk : 0u;                                      // the block's new rows
         const uint32_t r1 = len - jj * kBlk < (uint32_t)kBlk ? len - jj * kBlk : (uint32_t)kBlk;
         const bool whole = !turn_no && j < open;           // complete: the rows the ring holds are needed, too
+        const int64_t index = whole ? block_index(a.b, a.c, seq, head, j) : -1;          // (asked for with the rows)
         if (a.vec) load_block<T, 8>(a, s, before, head, slot, jj, r0, r1, whole, kt, vt);
         else load_block<T, 1>(a, s, before, head, slot, jj, r0, r1, whole, kt, vt);
         __syncthreads();
@@ -299,7 +310,6 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
         }
         __syncthreads();
         if (whole) {                                       // compress
-            const int64_t index = block_index(a.b, a.c, seq, head, j);
             if (index >= 0) {
                 uint32_t m[2] = {0u, 0u};
 #pragma unroll

@@ -1,5 +1,5 @@
 // Keys and values into the compressed cache and out of it again.  Bound by HBM for prompts, by a chain of memory round trips for single tokens.
-// 18792 tokens, 8 + 8 heads of 128, bf16: in 39 us (3.0 TB/s; 31 without the rotation), with 32 heads of queries 103 us (4.1 TB/s), out 21 us
+// 18792 tokens, 8 + 8 heads of 128, bf16: in 37 us (3.1 TB/s; 31 without the rotation), with 32 heads of queries 100 us (4.2 TB/s), out 21 us
 // (5.6 TB/s).  64 single tokens: in 7.5 us, 11.5 if all of them complete a block, out 3.5.
 #include "comet_cache.h"
 
@@ -135,6 +135,17 @@ __device__ void compress_block(const AppendArgs &a, const Seq &s, uint32_t befor
     };
     const auto first_of = [&](uint32_t c) { return c < rot_chunks ? chunk_at<8>(a.rope, c) : rot + 16u * (c - rot_chunks); };
     const auto second_of = [&](uint32_t c) { return c < rot_chunks ? chunk_second<8>(a.rope) : 8u; };
+    // The first item's steps and position are asked for before its rows: loads are waited for in their order, and the sines are computed
+    // while the rows are on their way.
+    const uint32_t row0 = tid / per_row, c0 = tid - row0 * per_row;
+    const bool turns = row0 < (uint32_t)kBlk && c0 < rot_chunks;
+    uint64_t step[8];
+    int32_t position = (int32_t)(j * kBlk + row0);
+    if (turns) {
+        if (a.rope.positions) position = a.rope.positions[token0 + (int32_t)row0];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) step[u] = a.rope.steps[c0 * 8u + u];
+    }
 #pragma unroll
     for (int n = 0; n < kMost; ++n) {
         const uint32_t i = tid + n * kCacheBlock, row = i / per_row, c = i - row * per_row;
@@ -154,13 +165,18 @@ __device__ void compress_block(const AppendArgs &a, const Seq &s, uint32_t befor
         }
     }
     const int64_t index = block_index(a.b, a.c, seq, head, j);           // (asked for behind the rows, waited for with them)
+    float sn[8], cs[8];
+    if (turns) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) turn_sincos(turn(position, step[u]), a.rope.amp, sn[u], cs[u]);
+    }
 #pragma unroll
     for (int n = 0; n < kMost; ++n) {
         const uint32_t i = tid + n * kCacheBlock, row = i / per_row, c = i - row * per_row;
         if (row < (uint32_t)kBlk) {
             if (c < rot_chunks) {
-                float x[8], y[8], sn[8], cs[8];
-                chunk_angles<8>(a.rope, c, a.rope.positions ? a.rope.positions[token0 + (int32_t)row] : (int32_t)(j * kBlk + row), 0u, sn, cs);
+                float x[8], y[8];
+                if (n) chunk_angles<8>(a.rope, c, a.rope.positions ? a.rope.positions[token0 + (int32_t)row] : (int32_t)(j * kBlk + row), 0u, sn, cs);
 #pragma unroll
                 for (int u = 0; u < 8; ++u) { x[u] = (float)ka[n][u]; y[u] = (float)kb[n][u]; }
                 chunk_turn<8>(a.rope.interleaved, x, y, sn, cs);

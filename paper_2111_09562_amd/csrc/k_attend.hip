@@ -5,7 +5,8 @@ namespace comet {
 
 // Few rows: a wavefront holds 32 rows (queries of one key/value head, its group's heads side by side) and goes through every fourth
 // block of its workgroup's piece straight from memory into the operands of the matrix instruction, with no LDS and no barrier
-// in the loop.  Bound by HBM as long as rows are few (64 sequences of 400 to 16384 tokens, 8 heads of 128, 4 rows each: 122 us, 4.3 TB/s).  grid: heads * pieces workgroups of kAttendBlock threads, the heads of a piece side by side
+// in the loop.  Bound by HBM as long as rows are few (64 sequences of 400 to 16384 tokens, 8 heads of 128, 4 rows each: 122 us, 4.3 TB/s).
+// grid: heads * pieces workgroups of kAttendBlock threads, the heads of a piece side by side
 template <int NC>
 __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(AttendArgs a) {
     constexpr uint32_t dim = 32u * NC;
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
 }
 
 // Fewer still: the same with tiles of 16 rows, half the registers and so twice the wavefronts and loads in flight.  Bound by HBM: the same sequences
-// 114 us (4.6 TB/s), two of 120000 tokens 91 us (5.4 TB/s; a large copy reaches 5.1); one of 701 tokens 7.6 us, a chain of memory round trips.
+// 109 us (4.8 TB/s), two of 120000 tokens 91 us (5.4 TB/s; a large copy reaches 5.1); one of 701 tokens 7.6 us, a chain of memory round trips.
 // EXACT: what rounding the weights to float16 leaves is multiplied as well, for results in float16 (whose own rounding is no larger: together 1.45 times
 // the error of one; the second product hides behind the loads).
 template <int NC, bool EXACT>

@@ -161,6 +161,33 @@ __device__ inline bool find_piece(const AttendArgs &a, uint32_t number, Piece *p
     return p->seq != 0xffffffffu;             // (a sequence whose numbers make no sense has no tiles)
 }
 
+// The last sequence whose units (first_unit) begin at or before `unit`, and which of its tiles that is, by all lanes of a wavefront: 64 candidates a
+// turn, once 64 are left everything about them at once.  false: none of its tiles.  Starts that do not grow give some sequence, never one out of range.
+__device__ inline bool find_tile(const AttendArgs &a, uint32_t unit, SeqWork *w, uint32_t *tile) {
+    uint32_t lo = 0, len = a.b.n_seqs;
+    while (len > 64u) {
+        const uint32_t stride = (len + 63u) / 64u, off = (uint32_t)lane_id() * stride;
+        const bool le = off < len && first_unit(a.b.starts, lo + off, a.group, a.tile_shift, 1u) <= unit;
+        const uint32_t n = (uint32_t)__popcll(wave_ballot(le)), k = n > 0u ? n - 1u : 0u;
+        lo += k * stride;
+        len = len - k * stride < stride ? len - k * stride : stride;
+    }
+    const uint32_t mine = (uint32_t)lane_id() < len ? lo + (uint32_t)lane_id() : lo;
+    SeqWork own;
+    own.read(a, mine);
+    const uint32_t first = first_unit(a.b.starts, mine, a.group, a.tile_shift, 1u);
+    const uint32_t n = (uint32_t)__popcll(wave_ballot((uint32_t)lane_id() < len && first <= unit));
+    const int k = (int)(n > 0u ? n - 1u : 0u);
+    w->tiles = lane_value(own.tiles, k);
+    w->blocks = lane_value(own.blocks, k);
+    w->s.start = (int32_t)lane_value((uint32_t)own.s.start, k);
+    w->s.n = (int32_t)lane_value((uint32_t)own.s.n, k);
+    w->s.len = (int32_t)lane_value((uint32_t)own.s.len, k);
+    const uint32_t f = lane_value(first, k);
+    *tile = unit - f;
+    return unit >= f && *tile < w->tiles;
+}
+
 // Eight whole numbers of 8 bits as float16: a byte u = v + 128 behind the byte 0x64 is the float16 number 1024 + u.
 __device__ inline half8 whole8(uint32_t lo, uint32_t hi) {
     lo ^= 0x80808080u;

@@ -219,21 +219,6 @@ __device__ inline void raise(int32_t *status) {
 __device__ inline uint32_t first_unit(const int32_t *starts, uint32_t b, uint32_t mul, uint32_t shift, uint32_t extra) {
     return (uint32_t)(((uint64_t)(uint32_t)starts[b] * mul) >> shift) + extra * b;
 }
-// The last sequence whose units begin at or before `unit`, by all lanes of a wavefront: 64 candidates a turn.  Starts
-// that do not grow give some sequence, never one out of range.
-__device__ inline uint32_t find_sequence(const int32_t *starts, uint32_t n_seqs, uint32_t unit, uint32_t mul, uint32_t shift, uint32_t extra) {
-    uint32_t lo = 0, len = n_seqs;
-    while (len > 1u) {
-        const uint32_t stride = (len + 63u) / 64u, off = (uint32_t)lane_id() * stride;
-        const bool le = off < len && first_unit(starts, lo + off, mul, shift, extra) <= unit;
-        const uint32_t n = (uint32_t)__popcll(wave_ballot(le));
-        const uint32_t k = n > 0u ? n - 1u : 0u;
-        lo += k * stride;
-        len = len - k * stride < stride ? len - k * stride : stride;
-    }
-    return (uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
-}
-
 struct Seq {
     int32_t start, n, len;      // first token in the batch, new tokens, tokens held once they are in
 };

@@ -112,8 +112,9 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
 
     while (j < end) {
         const uint32_t count = end - j < 64u ? end - j : 64u;
-        // In step i the keys of block i + 2 and the values of block i + 1 come into LDS, in the place of what was read in step i - 1;
-        // behind the last block it is staged again, and not used.
+        // In step i the keys of block i + 2 and the values of block i + 1 come into LDS, in the place of what was read before a barrier that every
+        // wavefront has passed since: that of step i - 1, or, for what is read in front of step 0, the one behind that read.  Behind the last block it
+        // is staged again, and not used.
         const auto at = [&](uint32_t i) {
             const int64_t index = look.index_of(i < count ? i : count - 1u);
             return index < 0 ? 0 : index;
@@ -139,6 +140,7 @@ __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_at
             half8 kk[2 * NC], vv[2 * NC], pa[2] = {}, pb[2] = {};
             operands(kk, 0, 0);
             f32x16 sa = products(kk, 0), sb = {};
+            __syncthreads();                                           // (step 0 puts the keys of block 2 where these were)
             if constexpr (RT == 1) operands(kk, 0, 1);
 #pragma unroll
             for (int c = 0; c < 2 * NC; ++c) vv[c] = half8{};

@@ -398,7 +398,12 @@ struct Lookup {
         ks = s[0];
         lb = s[1];
     }
-    __device__ void finish() { lb = log2_fast(lb); }
+    // Where there is no page the scales read are another block's, of which anything can be left, Inf among it: the block is not seen, and an
+    // ordinary scale keeps what is computed for it 0.
+    __device__ void finish() {
+        ks = index < 0 ? 0.0f : ks;
+        lb = index < 0 ? 0.0f : log2_fast(lb);
+    }
     __device__ void get(const AttendArgs &a, uint32_t seq, uint32_t head, uint32_t j, uint32_t end) {
         request(a, seq, head, j, end);
         finish();

@@ -1,0 +1,44 @@
+"""The compressed key/value cache where values lie next to a border: pages that are none, lengths set back more than once, values half way between
+two steps, weights next to a rounding, tensors that autograd knows.  Against 64 bits, as in test_gpu_cache."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+import cache_reference as ref  # noqa: E402
+from test_gpu_cache import DT, U32, Sequences, check_attend, check_held, comet, gen, rope_bound, u  # noqa: E402, F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- pages that are none ------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("stray", [math.inf, -math.inf, math.nan, 0.0, -1.0, 1.0])
+@pytest.mark.parametrize("dtype,group,new", [("bf16", 1, 1), ("fp16", 4, 1), ("bf16", 2, 7), ("fp16", 1, 16), ("bf16", 5, 5), ("fp16", 2, 32), ("bf16", 1, 64),
+                                             ("bf16", 3, 70), ("fp16", 1, 200)])
+def test_missing_pages(comet, dtype, group, new, stray):  # noqa: F811
+    """Tokens of a page that is none are not seen, however few the rows are, whatever lies in the cache where nobody has written."""
+    s = Sequences(comet, DT[dtype], 2, 64, 1, 1024, seed=new)
+    s.table = torch.arange(2, 2 + s.table.shape[1], dtype=torch.int32)[None]          # page 0 is nobody's
+    s.grow([900])
+    blocks = s.pages * 2 * 2
+    s.cache.buf[blocks * 64 * 64:blocks * (64 * 64 + 8)].view(torch.float32).view(s.pages, -1)[:2] = stray
+    q = s.tokens(new, 2 * group)
+    k, v = s.held(0)
+    for missing in ([0], [5], [3, 4, 12], [13]):                                     # the first, in the middle, several, the last with complete blocks
+        good = s.table.clone()
+        s.table[0, missing] = -1
+        s.status.zero_()
+        out, lse = s.cache.comet_cache_attend(s.batch([new]), q.cuda(), lse=True, status=s.status)
+        assert int(s.status.item()) == comet.ERR_FORMAT
+        s.table = good
+        keep = torch.ones(900, dtype=torch.bool)
+        for p in missing:
+            keep[64 * p:min(64 * p + 64, 896)] = False                               # (the open block is in the ring)
+        for i in sorted({0, new // 2, new - 1}):
+            seen = keep[:900 - new + i + 1].nonzero().flatten()
+            o, want, size, top = ref.attention(q[i:i + 1], k[:, seen], v[:, seen], 0.125, False)
+            d = 72 * U32 * top
+            assert ((lse[i].cpu().double() - want[0]).abs() <= d + 2.0 ** -18).all()
+            assert ((out[i].cpu().double() - o[0]).abs() <= ((u(torch.float16) + 2 * d + 2.0 ** -19) * size + u(s.dt) * o.abs() + 2.0 ** -24)[0]).all()

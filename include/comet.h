@@ -223,12 +223,15 @@ int comet_controller_update(comet_controller *c, const float *eb_old, const floa
  *   dev_table   int32[n_seqs][table_width]: the page of the tokens p * page_tokens ..; entries that are not reached are not read
  *   dev_slots   int32[n_seqs], or NULL for slot b
  * Two sequences of one append must not share a slot or a page that the call completes a block in (values undefined, never out of
- * bounds).  Complete blocks are never written again by tokens that follow, so sequences may share the pages of a
- * common beginning that ends with a block.  A sequence's length may be set back by up to 32 tokens (drafted tokens that are
- * not taken): the slot keeps the open block and the one before it.
+ * bounds).  Complete blocks are not written again by tokens that follow, so sequences may share the pages of a
+ * common beginning that ends with a block.  A sequence's length may be set back (drafted tokens that are not taken), as often as one likes, but
+ * never to less than 32 tokens below the greatest length it has had: the slot holds the block of the greatest length and the one
+ * before it in 16 bits, and what is older is gone (nothing tells the library, the values of the open block are then
+ * others').  A block that a set-back opens is written again when it is complete once more, so its page must not be shared.
  * Conditions known on the device only (rows outside the tensors, a page that is none, a slot that is none, lens[b] < n in an append or fetch) store
  * COMET_ERR_FORMAT in *dev_status if that is given, and leave it alone otherwise (the caller clears it); what they
- * touch is skipped: rows left as they were, tokens of a page that is none not seen.  A token whose key (value) holds Inf or NaN makes NaN of
+ * touch is skipped: rows left as they were, tokens of a page that is none not seen.  (starts that are outside of the rows or decrease may
+ * make a call skip other sequences' rows too.)  A token whose key (value) holds Inf or NaN makes NaN of
  * the keys (values) of its block and head when read back, and of the rows that see any of the block.
  *
  * Tensors are [tokens][heads][dim] with strides in elements; the dim values of a row are contiguous; in those that are written no two rows may overlap,

@@ -470,7 +470,8 @@ def comet_rope(x, rope: Rope, positions=None, out=None, backward: bool = False, 
 
 class Batch:
     """Which tokens of which sequences a call on a cache is about (int32 device tensors, read when the call runs): starts [n + 1], lens [n]
-    (tokens held once the batch's are in), table [n, pages], slots [n] or None."""
+    (tokens held once the batch's are in), table [n, pages], slots [n] or None.  A length may be set back between calls, never to less than
+    CACHE_BLOCK tokens below the greatest it has been, nor into a block of a page that another sequence shares."""
 
     def __init__(self, starts, lens, table, slots=None):
         dev = self.device_index = lens.get_device()

@@ -290,7 +290,7 @@ __global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
         return;
     }
     uint16_t *kt = s_rows, *vt = s_rows + kBlk * pitch;
-    // The ring keeps the open block and the one before it, so the length may be set back by up to a block.  A half that holds the
+    // The ring keeps the open block and the one before it, so the length may be set back to 32 tokens below the greatest it has been.  A half that holds the
     // beginning of block j0 is overwritten by a later block of the same parity: that one is left to the workgroup
     // of j0, which reads the half first.
     const bool leads = j == j0 && before % kBlk != 0u;

@@ -42,3 +42,27 @@ def test_missing_pages(comet, dtype, group, new, stray):  # noqa: F811
             d = 72 * U32 * top
             assert ((lse[i].cpu().double() - want[0]).abs() <= d + 2.0 ** -18).all()
             assert ((out[i].cpu().double() - o[0]).abs() <= ((u(torch.float16) + 2 * d + 2.0 ** -19) * size + u(s.dt) * o.abs() + 2.0 ** -24)[0]).all()
+
+
+# ---- lengths that are set back ------------------------------------------------------------------------------------
+
+
+def test_set_back_again(comet):  # noqa: F811
+    """Set back, grown, set back once more, never below 32 tokens under the greatest length: the open block is the tokens that came."""
+    for most, path in ((65, ((3, 1), (30, 40))), (70, ((20, 2), (13, 1), (1, 70))), (96, ((32, 5), (4, 40))), (127, ((1, 1), (32, 0), (0, 3), (3, 90)))):
+        s = Sequences(comet, torch.bfloat16, 2, 64, 1, 256, seed=most)
+        s.grow([most])
+        greatest = most
+        for back, new in path:
+            s.lens[0] -= back
+            assert s.lens[0] >= greatest - 32
+            s.k[0], s.v[0] = s.k[0][:s.lens[0]], s.v[0][:s.lens[0]]
+            check_held(s, 0)
+            q = s.tokens(1, 4)
+            out, lse = s.cache.comet_cache_attend(s.batch([1]), q.cuda(), lse=True, status=s.status)
+            check_attend(s, [1], q, out, lse)
+            if new:
+                s.grow([new])
+            greatest = max(greatest, s.lens[0])
+            check_held(s, 0)
+        assert s.ok()

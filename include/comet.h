@@ -235,7 +235,9 @@ int comet_controller_update(comet_controller *c, const float *eb_old, const floa
  * the keys (values) of its block and head when read back, and of the rows that see any of the block.
  *
  * Tensors are [tokens][heads][dim] with strides in elements; the dim values of a row are contiguous; in those that are written no two rows may overlap,
- * and the rows of a token lie between those of its neighbours, or the rows of a head (else COMET_ERR_INVALID).  dtype: COMET_F16 or COMET_BF16
+ * and the rows of a token lie between those of its neighbours, or the rows of a head (else COMET_ERR_INVALID).  No row of a result may overlap a row of
+ * another tensor of the call, unless the result is said to be allowed to be that tensor; two tensors that lie in one another's range (slices of one
+ * buffer) must have the same token stride, by which that is told (else COMET_ERR_INVALID).  dtype: COMET_F16 or COMET_BF16
  * (comet_rope: COMET_F32 too).  Everything is asynchronous on `stream` and may be captured into a HIP graph; a replay
  * goes by what the batch's arrays hold then.  Nothing is allocated. */
 #define COMET_F32 0
@@ -264,7 +266,7 @@ typedef struct { uint32_t rot, scaling; double base, factor, original_len, beta_
 int comet_rope_steps(const comet_rope_cfg *cfg, uint64_t *host_steps, float *amp);
 
 /* y = x turned by its tokens' positions (dev_positions: int32[n_tokens], or NULL for 0, 1, ..).  backward != 0: turned the other way, which
- * takes the gradient of y to that of x.  y may be x (same strides); else they must not overlap.  dim: any from rot on. */
+ * takes the gradient of y to that of x.  y may be x (same strides).  dim: any from rot on. */
 int comet_rope(const comet_rope_plan *plan, comet_rows x, comet_rows y, uint32_t n_tokens, uint32_t heads, uint32_t dim, int dtype,
                const int32_t *dev_positions, int backward, void *stream);
 
@@ -285,7 +287,7 @@ int comet_cache_fetch(const void *dev_cache, comet_cache_shape shape, const come
 /* Attention of the batch's queries over the cache: out = softmax(scale * q k^T) v, query heads h * q_heads/heads .. sharing key/value head h.
  * causal != 0: a query sees the tokens up to its own place (n queries are the last n of lens[b] tokens; those in front of
  * the first see nothing); 0: all lens[b].  A row that sees nothing is 0 and its lse -Inf.  dev_lse: float32[n_tokens][q_heads],
- * log of the sum of exp of the row's scores, or NULL.  out must not overlap q.  scale: finite, >= 0.  dev_work: comet_cache_attend_work bytes, 16-byte aligned, whose contents
+ * log of the sum of exp of the row's scores, or NULL.  scale: finite, >= 0.  dev_work: comet_cache_attend_work bytes, 16-byte aligned, whose contents
  * need no initialisation; calls that can overlap in time need one each. */
 uint64_t comet_cache_attend_work(comet_cache_shape shape, uint32_t n_seqs, uint32_t n_tokens, uint32_t q_heads);
 int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const comet_cache_batch *batch, uint32_t n_tokens, comet_rows q, uint32_t q_heads,

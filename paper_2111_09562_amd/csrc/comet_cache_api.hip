@@ -65,6 +65,49 @@ bool out_args(comet_rows r, int dtype, uint32_t tokens, uint32_t heads, uint32_t
     const bool tokens_apart = tokens < 2u || token >= head * (heads - 1u) + dim, heads_apart = heads < 2u || head >= token * (tokens - 1u) + dim;
     return rows_args(r, dtype, to) && (tokens < 2u || token >= dim) && (heads < 2u || head >= dim) && (tokens_apart || heads_apart);
 }
+// Whether no row of one tensor meets one of another of the same tokens, in bytes.  Told by their ranges, else row by row, for which the
+// token strides must be the same: rows of two heads then meet if some whole number of token strides lies near their distance.
+// A step over all pairs of heads is one over the distances if the head strides are the same, too.
+struct Span {
+    __int128 token, head, low, high;                       // high: behind the last byte
+    uint32_t heads;
+    Span(const Rows &r, uint32_t tokens, uint32_t heads_, uint32_t dim, uint32_t size) : heads(heads_) {
+        token = tokens < 2u ? 0 : (__int128)r.token * size;
+        head = heads < 2u ? 0 : (__int128)r.head * size;
+        const __int128 t = token * ((__int128)tokens - 1), h = head * ((__int128)heads - 1), at = (__int128)(uintptr_t)r.p;
+        low = at + (t < 0 ? t : 0) + (h < 0 ? h : 0);
+        high = at + (t > 0 ? t : 0) + (h > 0 ? h : 0) + (__int128)dim * size;
+    }
+};
+bool rows_apart(const Rows &x, uint32_t x_heads, const Rows &y, uint32_t y_heads, uint32_t tokens, uint32_t dim, int dtype) {
+    const uint32_t size = elem_size(dtype);
+    const Span a(x, tokens, x_heads, dim, size), b(y, tokens, y_heads, dim, size);
+    if (a.high <= b.low || b.high <= a.low) return true;
+    if (a.token != b.token) return false;
+    const __int128 length = (__int128)dim * size, base = (__int128)(uintptr_t)y.p - (__int128)(uintptr_t)x.p, step = a.token < 0 ? -a.token : a.token;
+    const auto meet = [&](__int128 distance) {             // |distance - m step| < length for some |m| < tokens
+        if (distance < 0) distance = -distance;
+        if (!step) return distance < length;
+        __int128 m = distance / step;
+        if (m > (__int128)tokens - 1) m = (__int128)tokens - 1;
+        return distance - m * step < length || (m + 1 < (__int128)tokens && (m + 1) * step - distance < length);
+    };
+    if (a.head == b.head || x_heads < 2u || y_heads < 2u) {
+        const __int128 head = x_heads < 2u ? b.head : a.head;
+        for (int64_t d = -(int64_t)(x_heads - 1u); d <= (int64_t)(y_heads - 1u); ++d)
+            if (meet(base + d * head)) return false;
+        return true;
+    }
+    if ((uint64_t)x_heads * y_heads > (1u << 20)) return false;
+    for (uint32_t g = 0; g < y_heads; ++g)
+        for (uint32_t h = 0; h < x_heads; ++h)
+            if (meet(base + g * b.head - h * a.head)) return false;
+    return true;
+}
+// A result and what it is computed from, which may be the same tensor.
+bool same_or_apart(const Rows &x, const Rows &y, uint32_t heads, uint32_t tokens, uint32_t dim, int dtype) {
+    return x.p == y.p ? x.token == y.token && x.head == y.head : rows_apart(x, heads, y, heads, tokens, dim, dtype);
+}
 bool rows_aligned(const Rows &r, int dtype) {                                   // every row begins at a multiple of 16 bytes
     const int64_t v = 16 / elem_size(dtype);
     return (uintptr_t)r.p % 16u == 0u && r.token % v == 0 && r.head % v == 0;
@@ -194,7 +237,7 @@ int comet_rope(const comet_rope_plan *plan, comet_rows x, comet_rows y, uint32_t
     if (!n_tokens) return COMET_OK;
     if (!rows_args(x, dtype, &rx) || !out_args(y, dtype, n_tokens, heads, dim, &ry)) return COMET_ERR_INVALID;
     const bool in_place = x.dev == y.dev;
-    if (in_place && (x.token_stride != y.token_stride || x.head_stride != y.head_stride)) return COMET_ERR_INVALID;
+    if (!same_or_apart(rx, ry, heads, n_tokens, dim, dtype)) return COMET_ERR_INVALID;
     const uint32_t v = 16u / elem_size(dtype);
     const bool vec = r.rot % (2u * v) == 0u && (dim - r.rot) % v == 0u && rows_aligned(rx, dtype) && rows_aligned(ry, dtype);
     const uint32_t sign = backward ? 0x80000000u : 0u;
@@ -232,7 +275,8 @@ int comet_cache_append(void *dev_cache, comet_cache_shape shape, const comet_cac
     uint32_t q_wg = 0;
     if (q_heads) {
         if (!rows_args(q, dtype, &a.q) || !out_args(q_out, dtype, n_tokens, q_heads, shape.dim, &a.q_out)) return COMET_ERR_INVALID;
-        if (q.dev == q_out.dev && (q.token_stride != q_out.token_stride || q.head_stride != q_out.head_stride)) return COMET_ERR_INVALID;
+        if (!same_or_apart(a.q, a.q_out, q_heads, n_tokens, shape.dim, dtype) || !rows_apart(a.k, shape.heads, a.q_out, q_heads, n_tokens, shape.dim, dtype) ||
+            !rows_apart(a.v, shape.heads, a.q_out, q_heads, n_tokens, shape.dim, dtype)) return COMET_ERR_INVALID;
         a.vec = a.vec && rows_aligned(a.q, dtype) && rows_aligned(a.q_out, dtype);
         a.q_heads_wg = 8u;
         q_wg = (q_heads + a.q_heads_wg - 1u) / a.q_heads_wg;
@@ -251,7 +295,8 @@ int comet_cache_fetch(const void *dev_cache, comet_cache_shape shape, const come
     if ((dtype != COMET_F16 && dtype != COMET_BF16) || !cache_args(dev_cache, shape, &a.c) || !batch_args(batch, n_tokens, dev_status, &a.b))
         return COMET_ERR_INVALID;
     if (!n_tokens) return COMET_OK;
-    if (!out_args(k, dtype, n_tokens, shape.heads, shape.dim, &a.k) || !out_args(v, dtype, n_tokens, shape.heads, shape.dim, &a.v)) return COMET_ERR_INVALID;
+    if (!out_args(k, dtype, n_tokens, shape.heads, shape.dim, &a.k) || !out_args(v, dtype, n_tokens, shape.heads, shape.dim, &a.v) ||
+        !rows_apart(a.k, shape.heads, a.v, shape.heads, n_tokens, shape.dim, dtype)) return COMET_ERR_INVALID;
     a.vec = rows_aligned(a.k, dtype) && rows_aligned(a.v, dtype);
     const dim3 grid(block_units(a.b), shape.heads);
     hipStream_t st = (hipStream_t)stream;
@@ -275,8 +320,8 @@ int comet_cache_attend(const void *dev_cache, comet_cache_shape shape, const com
         !std::isfinite(scale * 1.4426950408889634f) || scale < 0.0f || (uintptr_t)dev_lse % 4u || !plan_attend(shape, batch->n_seqs, n_tokens, q_heads, &p))
         return COMET_ERR_INVALID;
     if (!n_tokens) return COMET_OK;
-    if (!rows_args(q, dtype, &a.q) || !out_args(out, dtype, n_tokens, q_heads, shape.dim, &a.out) || q.dev == out.dev || !dev_work || (uintptr_t)dev_work % 16u)
-        return COMET_ERR_INVALID;
+    if (!rows_args(q, dtype, &a.q) || !out_args(out, dtype, n_tokens, q_heads, shape.dim, &a.out) ||
+        !rows_apart(a.q, q_heads, a.out, q_heads, n_tokens, shape.dim, dtype) || !dev_work || (uintptr_t)dev_work % 16u) return COMET_ERR_INVALID;
     if (work_bytes < p.bytes) return COMET_ERR_NOMEM;
     a.lse = dev_lse; a.q_heads = q_heads; a.group = q_heads / shape.heads;
     a.bf16 = dtype == COMET_BF16; a.causal = causal != 0; a.wide = p.wide; a.vec = rows_aligned(a.q, dtype) && rows_aligned(a.out, dtype);

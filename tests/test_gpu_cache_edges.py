@@ -66,3 +66,34 @@ def test_set_back_again(comet):  # noqa: F811
             greatest = max(greatest, s.lens[0])
             check_held(s, 0)
         assert s.ok()
+
+
+# ---- operands in one buffer ----------------------------------------------------------------------------------------
+
+
+def test_operands_side_by_side(comet):  # noqa: F811
+    """Results between the operands in one buffer, where rows do not meet, give what they give elsewhere."""
+    s = Sequences(comet, torch.float16, 2, 64, 2, 128, rope=comet.Rope(64), seed=8)
+    s.grow([50, 20])
+    new, tokens = [3, 1], 4
+    fused = torch.randn(tokens, 4 + 2 + 2 + 4, 64, generator=s.g).half().cuda()          # queries, keys, values, room for the results
+    q, k, v, room = fused[:, :4], fused[:, 4:6], fused[:, 6:8], fused[:, 8:]
+    for b, n in enumerate(new):
+        s.lens[b] += n
+    batch = s.batch(new)
+    want = s.cache.comet_cache_append(batch, k, v, rope=s.rope, q=q)
+    s.cache.comet_cache_append(batch, k, v, rope=s.rope, q=q, q_out=room)
+    assert torch.equal(room, want)
+    want = s.cache.comet_cache_attend(batch, q)
+    s.cache.comet_cache_attend(batch, q, out=room)
+    assert torch.equal(room, want)
+    pairs = torch.randn(tokens, 2, 4, 64, generator=s.g).half().cuda()                    # head by head: keys of the strides of the values
+    wk, wv = s.cache.comet_cache_fetch(batch, dtype=s.dt, tokens=tokens)
+    s.cache.comet_cache_fetch(batch, pairs[:, :, 0], pairs[:, :, 2])
+    assert torch.equal(pairs[:, :, 0], wk) and torch.equal(pairs[:, :, 2], wv)
+    want = comet.comet_rope(q, s.rope)
+    comet.comet_rope(q, s.rope, out=room)
+    assert torch.equal(room, want)
+    by_head = torch.zeros(4, 16, 64, dtype=s.dt, device="cuda")                           # [head][token], other strides than the input's
+    comet.comet_rope(q, s.rope, out=by_head[:, :tokens].transpose(0, 1))
+    assert torch.equal(by_head[:, :tokens].transpose(0, 1), want)

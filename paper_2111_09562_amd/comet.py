@@ -378,6 +378,24 @@ def _elsewhere(dev: int, stream):
     return torch.cuda.stream(stream)                 # (makes the stream's device current, too)
 
 
+def _no_gradient(where: str, *tensors) -> None:
+    """These calls have no gradient: where one is asked for they would lose it without a word."""
+    for t in tensors:
+        if t is not None and t is not True and t.requires_grad:
+            import torch
+            if torch.is_grad_enabled():
+                raise RuntimeError(f"{where}: a tensor asks for a gradient, which this call does not have (a rotation has one in autograd.rotate; "
+                                   "detach the tensor, or call under torch.no_grad())")
+
+
+def _written(*tensors) -> None:
+    """Tells autograd that tensors of the caller were written: a graph that saved one refuses its backward pass."""
+    import torch
+    tensors = [t for t in tensors if t is not None and not t.is_inference()]
+    if tensors:
+        torch.autograd.graph.increment_version(tensors)
+
+
 def _raw_stream(dev: int) -> int:
     import torch
     return torch._C._cuda_getCurrentRawStream(dev)
@@ -448,7 +466,8 @@ class Rope:
 
 def comet_rope(x, rope: Rope, positions=None, out=None, backward: bool = False, stream=None):
     """x [tokens, heads, dim] (fp32, fp16 or bf16, any strides with contiguous heads) turned by its tokens' positions (int32, or None for
-    0, 1, ..); backward: the other way.  out: the result's tensor, x itself is fine."""
+    0, 1, ..); backward: the other way.  out: the result's tensor, x itself is fine.  Has no gradient (``autograd.rotate`` has)."""
+    _no_gradient("comet_rope", x, out)
     dev = x.get_device()
     on = _elsewhere(dev, stream)
     if on is not None:
@@ -458,6 +477,7 @@ def comet_rope(x, rope: Rope, positions=None, out=None, backward: bool = False, 
         raise ValueError(f"comet_rope: x [tokens, heads, dim] expected, got {tuple(x.shape)}")
     tokens, heads, dim = x.shape
     rx = _rows3(x, "comet_rope: x", dev, tokens, heads, dim, x.dtype)
+    given = out
     if out is None:
         out = x.new_empty((tokens, heads, dim))
     ry = _rows3(out, "comet_rope: out", dev, tokens, heads, dim, x.dtype)
@@ -465,6 +485,8 @@ def comet_rope(x, rope: Rope, positions=None, out=None, backward: bool = False, 
         raise ValueError("comet_rope: the rotation's steps are on another device")
     pos = None if positions is None else _int32(positions, "comet_rope: positions", dev, tokens)
     _chk(lib().comet_rope(rope._plan, rx, ry, tokens, heads, dim, _row_dtype(x), pos, 1 if backward else 0, _raw_stream(dev)), "comet_rope")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -508,13 +530,14 @@ class Cache:
 
     def comet_cache_append(self, batch: Batch, k, v, rope: Rope | None = None, q=None, q_out=None, positions=None, status=None, stream=None):
         """Put the batch's keys and values [tokens, heads, dim] (fp16 or bf16) into the cache, the keys turned by `rope` on the way.
-        q [tokens, query heads, dim]: turned as well, into q_out (a new tensor if None), which is returned."""
+        q [tokens, query heads, dim]: turned as well, into q_out (a new tensor if None; q itself is fine), which is returned.  Has no gradient."""
+        _no_gradient("comet_cache_append", k, v, q, q_out)
         dev = self._same("comet_cache_append", batch, rope)
         on = _elsewhere(dev, stream)
         if on is not None:
             with on:
                 return self.comet_cache_append(batch, k, v, rope, q, q_out, positions, status)
-        tokens, dt, dim = k.shape[0], k.dtype, self.dim
+        tokens, dt, dim, given = k.shape[0], k.dtype, self.dim, q_out
         rk = _rows3(k, "comet_cache_append: k", dev, tokens, self.heads, dim, dt)
         rv = _rows3(v, "comet_cache_append: v", dev, tokens, self.heads, dim, dt)
         if q is not None:
@@ -531,12 +554,15 @@ class Cache:
         pos = None if positions is None else _int32(positions, "comet_cache_append: positions", dev, tokens)
         _chk(lib().comet_cache_append(self._p, self.shape, batch._c, tokens, rk, rv, rq, ro, q_heads, _dtype16(k), None if rope is None else rope._plan,
                                       pos, _raw_stream(dev), _status_ptr(status, dev)), "comet_cache_append")
+        if given is not None:
+            _written(given)
         return q_out
 
     def comet_cache_fetch(self, batch: Batch, k=None, v=None, dtype=None, tokens: int | None = None, status=None, stream=None):
         """The batch's keys and values as the cache holds them, (k, v): into the tensors given, or new ones of `dtype` with `tokens` rows (those
         that belong to no sequence stay as the allocator left them)."""
         import torch
+        _no_gradient("comet_cache_fetch", k, v)
         dev = self._same("comet_cache_fetch", batch)
         on = _elsewhere(dev, stream)
         if on is not None:
@@ -546,6 +572,7 @@ class Cache:
         if given is not None:
             tokens = given.shape[0] if tokens is None else tokens
             dtype = given.dtype if dtype is None else dtype
+        written = (k, v)
         if tokens is None or dtype is None:
             raise ValueError("comet_cache_fetch: tokens and dtype, or tensors for the result, expected")
         if k is None:
@@ -556,14 +583,17 @@ class Cache:
         rv = _rows3(v, "comet_cache_fetch: v", dev, tokens, self.heads, self.dim, dtype)
         _chk(lib().comet_cache_fetch(self._p, self.shape, batch._c, tokens, rk, rv, _dtype16(k), _raw_stream(dev), _status_ptr(status, dev)),
              "comet_cache_fetch")
+        if given is not None:
+            _written(*written)
         return k, v
 
     def comet_cache_attend(self, batch: Batch, q, out=None, lse=None, scale: float | None = None, causal: bool = True, work=None, status=None,
                            stream=None):
         """Attention of the batch's queries [tokens, query heads, dim] over the cache; scale: 1 / sqrt(dim) if None.  lse: a float32 tensor
         [tokens, query heads] for the log-sum-exp of every row, or True for a new one; then (out, lse) is returned, else out.  work: uint8 tensor
-        of comet_cache_attend_work bytes, allocated if None."""
+        of comet_cache_attend_work bytes, allocated if None.  Has no gradient."""
         import torch
+        _no_gradient("comet_cache_attend", q, out, lse)
         dev = self._same("comet_cache_attend", batch)
         on = _elsewhere(dev, stream)
         if on is not None:
@@ -572,6 +602,7 @@ class Cache:
         tokens, dt, dim = q.shape[0], q.dtype, self.dim
         rq = _rows3(q, "comet_cache_attend: q", dev, tokens, None, dim, dt)
         q_heads = q.shape[1]
+        given = (out, None if lse is True else lse)
         if out is None:
             out = q.new_empty((tokens, q_heads, dim))
         ro = _rows3(out, "comet_cache_attend: out", dev, tokens, q_heads, dim, dt)
@@ -590,6 +621,8 @@ class Cache:
         _chk(L.comet_cache_attend(self._p, self.shape, batch._c, tokens, rq, q_heads, _dtype16(q), dim ** -0.5 if scale is None else scale,
                                   1 if causal else 0, ro, None if lse is None else lse.data_ptr(), work.data_ptr(),
                                   work.numel() * work.element_size(), _raw_stream(dev), _status_ptr(status, dev)), "comet_cache_attend")
+        if given[0] is not None or given[1] is not None:
+            _written(*given)
         return out if lse is None else (out, lse)
 
 

@@ -82,3 +82,13 @@ def test_far_strides_do_not_overflow(comet):  # noqa: F811
         for at in (64, -64):
             assert attend(comet, (0, token, head), (at, 64, 32), 2, 4, 32) in (comet.ERR_INVALID, comet.ERR_NOMEM)
     assert attend(comet, (0, high, 32), (64, 64, 32), 2, 1, 32) == comet.ERR_NOMEM        # (one token has no stride)
+
+
+def test_rotation_refuses_what_asks_for_a_gradient(comet):  # noqa: F811
+    import torch
+    rope = comet.Rope(64, device="cpu")
+    for kw in (dict(), dict(out=torch.zeros(2, 2, 64, requires_grad=True))):
+        with pytest.raises(RuntimeError, match="gradient"):
+            comet.comet_rope(torch.zeros(2, 2, 64, requires_grad=not kw), rope, **kw)
+    with torch.no_grad(), pytest.raises(ValueError):                                      # (a host tensor)
+        comet.comet_rope(torch.zeros(2, 2, 64, requires_grad=True), rope)

@@ -97,3 +97,57 @@ def test_operands_side_by_side(comet):  # noqa: F811
     by_head = torch.zeros(4, 16, 64, dtype=s.dt, device="cuda")                           # [head][token], other strides than the input's
     comet.comet_rope(q, s.rope, out=by_head[:, :tokens].transpose(0, 1))
     assert torch.equal(by_head[:, :tokens].transpose(0, 1), want)
+
+
+# ---- tensors that autograd knows ----------------------------------------------------------------------------------
+
+
+def test_gradients_are_not_lost(comet):  # noqa: F811
+    """Calls that have no gradient refuse tensors that ask for one; what they write is known to autograd as written."""
+    from paper_2111_09562_amd import autograd
+    s = Sequences(comet, torch.bfloat16, 2, 64, 2, 128, rope=comet.Rope(64), seed=3)
+    s.grow([40, 3])
+    batch = s.batch([1, 1])
+    asks = lambda heads: s.tokens(2, heads).cuda().requires_grad_()  # noqa: E731
+    plain = lambda heads: s.tokens(2, heads).cuda()  # noqa: E731
+    before = s.cache.buf.clone()
+    k, q = plain(2), plain(4)
+    for call in (lambda: comet.comet_rope(asks(2), s.rope), lambda: comet.comet_rope(k, s.rope, out=asks(2)),
+                 lambda: s.cache.comet_cache_append(batch, asks(2), k), lambda: s.cache.comet_cache_append(batch, k, asks(2)),
+                 lambda: s.cache.comet_cache_append(batch, k, k, q=asks(4)), lambda: s.cache.comet_cache_append(batch, k, k, q=q, q_out=asks(4)),
+                 lambda: s.cache.comet_cache_fetch(batch, asks(2), k), lambda: s.cache.comet_cache_fetch(batch, k, asks(2)),
+                 lambda: s.cache.comet_cache_attend(batch, asks(4)), lambda: s.cache.comet_cache_attend(batch, q, out=asks(4)),
+                 lambda: s.cache.comet_cache_attend(batch, q, lse=torch.zeros(2, 4, device="cuda", requires_grad=True))):
+        with pytest.raises(RuntimeError, match="gradient"):
+            call()
+    assert torch.equal(s.cache.buf, before)
+    x = asks(2)
+    with torch.no_grad():                     # where nobody asks for gradients they go through
+        y = comet.comet_rope(x, s.rope)
+        s.cache.comet_cache_attend(batch, asks(4))
+    assert not y.requires_grad and autograd.rotate(x, s.rope).requires_grad
+    with torch.inference_mode():
+        a, b = s.tokens(2, 2).cuda(), s.tokens(2, 4).cuda()
+        comet.comet_rope(a, s.rope, out=a)
+        s.cache.comet_cache_fetch(batch, a, torch.empty_like(a))
+        s.cache.comet_cache_append(batch, a, a, q=b, q_out=b)
+        s.cache.comet_cache_attend(batch, b, out=torch.empty_like(b), lse=torch.empty(2, 4, device="cuda"))
+
+    def written(t):
+        """Saves t for a backward pass, writes it with the call that is given back's argument, and says whether the pass is refused."""
+        w = torch.ones_like(t, requires_grad=True)
+        z = (w * t).sum()
+        yield t
+        with pytest.raises(RuntimeError, match="inplace"):
+            z.backward()
+
+    out, lse, x = plain(4), torch.zeros(2, 4, device="cuda"), plain(2)
+    for tensors, call in (([x], lambda: comet.comet_rope(x, s.rope, out=x)), ([x, k], lambda: s.cache.comet_cache_fetch(batch, x, k)),
+                          ([out], lambda: s.cache.comet_cache_append(batch, k, k, q=q, q_out=out)), ([q], lambda: s.cache.comet_cache_append(batch, k, k, q=q, q_out=q)),
+                          ([out, lse], lambda: s.cache.comet_cache_attend(batch, q, out=out, lse=lse))):
+        open_graphs = [written(t) for t in tensors]
+        for graph in open_graphs:
+            next(graph)
+        call()
+        for graph in open_graphs:
+            assert next(graph, None) is None

@@ -68,6 +68,46 @@ def test_set_back_again(comet):  # noqa: F811
         assert s.ok()
 
 
+# ---- whole numbers half way between two ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("cuts", [[256], [16, 200, 40], [31, 1, 224], [1] * 33 + [223]])
+def test_whole_numbers(comet, dtype, cuts):  # noqa: F811
+    """x / s with s = max|x| / 127 rounded to the nearest whole number, ties to even, for all of a type's significands as the largest value.  In 64
+    bits 127 x and ties are exact, and everything else is at least 2^-19 of itself away from one: with x = m 2^e and a = n 2^f, m and n of at most 11 bits,
+    |254 x / a - odd| is a multiple of 2^(e - f) / n, and 2^e is at least x 2^-11.  (There are ties at x = a / 2, and others where n is a multiple of 127.)"""
+    heads, dim = 128, 32
+    s = Sequences(comet, DT[dtype], heads, dim, 1, 256, seed=7)
+    bits = 10 if dtype == "fp16" else 7
+    g = gen(70)
+    order = torch.randperm(8 * heads, generator=g)                                    # block and head -> significand of its largest value
+    largest = ((2.0 ** bits + order % 2 ** bits) * 2.0 ** -bits * 2.0 ** torch.randint(-10, 11, order.shape, generator=g)).view(8, 1, heads, 1)
+
+    def some():
+        x = ((torch.rand(8, 32, heads, dim, generator=g) * 2 - 1) * largest).to(DT[dtype]).double()
+        pick = torch.rand(x.shape, generator=g)
+        sign = torch.where(torch.rand(x.shape, generator=g) < 0.5, -1.0, 1.0)
+        x = torch.where(pick < 0.3, sign * largest / 2, x)                            # half way between 63 and 64
+        x = torch.where(pick > 0.98, sign * largest, x)
+        steps = torch.randint(-127, 128, x.shape, generator=g) + 0.5
+        x = torch.where((pick > 0.9) & (pick < 0.98), (steps * largest / 127.5).to(DT[dtype]).double(), x)
+        half = (sign * (torch.randint(0, 127, x.shape, generator=g) + 0.5) * largest / 127).to(DT[dtype]).double()
+        x = torch.where((pick > 0.5) & (pick < 0.8) & (254 * half % largest == 0), half, x)          # (where that is a number of the type)
+        x[:, 5, :, 3] = largest[:, 0, :, 0]
+        return x.view(256, heads, dim)
+
+    k, v = some(), some()
+    at = 0
+    for n in cuts:
+        s.grow([n], k=k[at:at + n].to(s.dt), v=v[at:at + n].to(s.dt))
+        at += n
+    scales = (largest / 127).expand(8, 32, heads, 1).reshape(256, heads, 1)
+    for got, x in zip(s.held(0), (k, v)):
+        got = got.transpose(0, 1) / scales                                            # (the cache's scale is off by 2^-24 of itself)
+        assert torch.equal(got.round(), torch.round(127 * x.view(8, 32, heads, dim) / largest).view_as(x))
+
+
 # ---- operands in one buffer ----------------------------------------------------------------------------------------
 
 

@@ -101,7 +101,7 @@ struct AttendArgs {
     float *part_s;                            // [slot][head][tile_rows][3]: reference and sum of the weights, reference of the values
     int32_t *directory;                       // [tile][2]: first slot, number of pieces
 };
-template <int NC>
+template <int NC, bool EXACT>
 __global__ void k_attend(AttendArgs a);
 template <int NC, bool EXACT>
 __global__ void k_attend_few(AttendArgs a);

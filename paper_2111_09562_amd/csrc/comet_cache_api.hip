@@ -195,7 +195,8 @@ void launch_attend(const AttendArgs &a, const AttendPlan &p, uint32_t wg, hipStr
         }
     if (p.few && a.bf16) k_attend_few<NC, false><<<wg, kAttendBlock, 0, st>>>(a);
     else if (p.few) k_attend_few<NC, true><<<wg, kAttendBlock, 0, st>>>(a);
-    else k_attend<NC><<<wg, kAttendBlock, 0, st>>>(a);
+    else if (a.bf16) k_attend<NC, false><<<wg, kAttendBlock, 0, st>>>(a);
+    else k_attend<NC, true><<<wg, kAttendBlock, 0, st>>>(a);
 }
 
 }  // namespace

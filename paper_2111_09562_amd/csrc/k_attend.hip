@@ -5,9 +5,12 @@ namespace comet {
 
 // Few rows: a wavefront holds 32 rows (queries of one key/value head, its group's heads side by side) and goes through every fourth
 // block of its workgroup's piece straight from memory into the operands of the matrix instruction, with no LDS and no barrier
-// in the loop.  Bound by HBM as long as rows are few (64 sequences of 400 to 16384 tokens, 8 heads of 128, 4 rows each: 122 us, 4.3 TB/s).
+// in the loop.  Bound by HBM and the conversion to float16 together (64 sequences of 400 to 16384 tokens, 8 heads of 128, 32 rows each: 155 us with the
+// join, 3.5 TB/s).
+// EXACT: what rounding the weights to float16 leaves is multiplied as well, for results in float16, as in k_attend_few (the same sequences
+// 161 us, 156 without; 48 sequences of up to 4096 tokens, 12 heads of 64, 20 rows each 39 us and 37).
 // grid: heads * pieces workgroups of kAttendBlock threads, the heads of a piece side by side
-template <int NC>
+template <int NC, bool EXACT>
 __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(AttendArgs a) {
     constexpr uint32_t dim = 32u * NC;
     __shared__ float s_stat[4][3][32];
@@ -61,7 +64,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
             }
             if (next >= 0) load(kr, next, 0u);
             const float kc = Lookup::of(look.ks, i) * qc, lb = Lookup::of(look.lb, i);
-            half8 pw[2];
+            half8 pw[2], rest[2] = {};
             // (one place that moves the references, and x once more behind it: two such places cost a hundred registers)
             const bool all = at >= 0 && (int32_t)(j * 32u + 32u) <= least && lb == lb;
             const int32_t limit = at >= 0 ? place.limit : 0;
@@ -78,16 +81,21 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
             }
             row.follow(top, tope);
             if (all) {
-                row.weights(acc, kc, lb, pw);
+                row.weights(acc, kc, lb, pw, EXACT ? rest : nullptr);
             } else {
                 float x[16];
                 some_of_block<32>(acc, kc, lb, j, limit, x, &top, &tope);
-                row.weights_some(x, lb, pw);
+                row.weights_some(x, lb, pw, EXACT ? rest : nullptr);
             }
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                row.o[c] = mfma(whole8(vr[c][0], vr[c][1]), pw[0], row.o[c]);
-                row.o[c] = mfma(whole8(vr[c][2], vr[c][3]), pw[1], row.o[c]);
+                const half8 v0 = whole8(vr[c][0], vr[c][1]), v1 = whole8(vr[c][2], vr[c][3]);
+                row.o[c] = mfma(v0, pw[0], row.o[c]);
+                row.o[c] = mfma(v1, pw[1], row.o[c]);
+                if constexpr (EXACT) {
+                    row.o[c] = mfma(v0, rest[0], row.o[c]);
+                    row.o[c] = mfma(v1, rest[1], row.o[c]);
+                }
             }
             if (next >= 0) load(vr, next, 1u);
             at = next;
@@ -115,13 +123,16 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
             float x[16], lv[16], top, tope;
             each_of_open<32>(acc, qc, reinterpret_cast<const float *>(half + 128ull * dim), held, j, place.limit, x, lv, &top, &tope);
             row.follow(top, tope);
-            half8 pw[2];
-            row.weights_each(x, lv, pw);
+            half8 pw[2], rest[2];
+            row.weights_each(x, lv, pw, EXACT ? rest : nullptr);
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    row.o[c] = mfma(open_values(half + 64u * dim + 2048u * c + 64u * n + 32u * h + 16u * u, u, held), pw[u], row.o[c]);
+                for (int u = 0; u < 2; ++u) {
+                    const half8 v = open_values(half + 64u * dim + 2048u * c + 64u * n + 32u * h + 16u * u, u, held);
+                    row.o[c] = mfma(v, pw[u], row.o[c]);
+                    if constexpr (EXACT) row.o[c] = mfma(v, rest[u], row.o[c]);
+                }
         }
     }
 
@@ -461,14 +472,22 @@ __global__ __launch_bounds__(kAttendBlock) void k_attend_join_tile(AttendArgs a)
     }
 }
 
-template __global__ void k_attend<1>(AttendArgs);
-template __global__ void k_attend<2>(AttendArgs);
-template __global__ void k_attend<3>(AttendArgs);
-template __global__ void k_attend<4>(AttendArgs);
-template __global__ void k_attend<5>(AttendArgs);
-template __global__ void k_attend<6>(AttendArgs);
-template __global__ void k_attend<7>(AttendArgs);
-template __global__ void k_attend<8>(AttendArgs);
+template __global__ void k_attend<1, false>(AttendArgs);
+template __global__ void k_attend<1, true>(AttendArgs);
+template __global__ void k_attend<2, false>(AttendArgs);
+template __global__ void k_attend<2, true>(AttendArgs);
+template __global__ void k_attend<3, false>(AttendArgs);
+template __global__ void k_attend<3, true>(AttendArgs);
+template __global__ void k_attend<4, false>(AttendArgs);
+template __global__ void k_attend<4, true>(AttendArgs);
+template __global__ void k_attend<5, false>(AttendArgs);
+template __global__ void k_attend<5, true>(AttendArgs);
+template __global__ void k_attend<6, false>(AttendArgs);
+template __global__ void k_attend<6, true>(AttendArgs);
+template __global__ void k_attend<7, false>(AttendArgs);
+template __global__ void k_attend<7, true>(AttendArgs);
+template __global__ void k_attend<8, false>(AttendArgs);
+template __global__ void k_attend<8, true>(AttendArgs);
 template __global__ void k_attend_few<1, false>(AttendArgs);
 template __global__ void k_attend_few<1, true>(AttendArgs);
 template __global__ void k_attend_few<2, false>(AttendArgs);

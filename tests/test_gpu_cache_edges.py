@@ -108,6 +108,33 @@ def test_whole_numbers(comet, dtype, cuts):  # noqa: F811
         assert torch.equal(got.round(), torch.round(127 * x.view(8, 32, heads, dim) / largest).view_as(x))
 
 
+# ---- weights next to a rounding -----------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dim,group,new", [(32, 1, [1, 1]), (32, 4, [1, 4]), (32, 1, [20, 40]), (64, 2, [9, 30]), (96, 3, [7, 12]), (32, 8, [5, 8]), (128, 4, [8, 16]),
+                                           (160, 1, [33, 17]), (256, 2, [16, 30])])
+def test_weights_of_float16_results(comet, dim, group, new):  # noqa: F811
+    """Up to 64 rows: results in float16 are as exact as float32 sums rounded once.  What rounding a weight to float16 leaves is multiplied too, so a
+    weight is off by 2^-22 of itself and by 2^-25, where the largest is 2^7 at least: 2^-32 of it for each of 100 tokens, together below 2^-25
+    of the largest value.  Scores are below 2 in magnitude, so d (see test_gpu_cache) is below (dim + 8) 2^-23."""
+    s = Sequences(comet, torch.float16, 2, dim, 2, 160, seed=dim + group)
+    held = [100 - n for n in new]
+    s.grow(held)
+    s.grow(new)
+    q = (s.tokens(sum(new), 2 * group) * (0.5 / math.sqrt(dim))).half()
+    out = s.cache.comet_cache_attend(s.batch(new), q.cuda())
+    at = 0
+    for b, n in enumerate(new):
+        k, v = s.held(b)
+        o, _, size, top = ref.attention(q[at:at + n], k, v, dim ** -0.5, True)
+        assert top < 2
+        d = (dim + 8) * U32 * top
+        tol = (2.0 ** -22 + 2 * d + 2.0 ** -20) * size + u(s.dt) * o.abs() + 2.0 ** -25 * v.abs().max() + 2.0 ** -25
+        off = (out[at:at + n].cpu().double() - o).abs()
+        assert (off <= tol).all(), float((off / tol).max())
+        at += n
+
+
 # ---- operands in one buffer ----------------------------------------------------------------------------------------
 
 

@@ -452,12 +452,17 @@ def comet_rope_steps(rot: int, base: float = 10000.0, scaling: str = "none", fac
 
 class Rope:
     """A rotation by positions, its steps in device memory: the first `rot` values of a head in pairs (i, i + rot/2), or (2i, 2i + 1)
-    if interleaved; scaling "none", "linear", "base" or "parts" for contexts `factor` times as long as original_len."""
+    if interleaved; scaling "none", "linear", "base" or "parts" for contexts `factor` times as long as original_len.  amp: the factor on the
+    turned values, if it is not to be the scaling's own (1 but for "parts")."""
 
     def __init__(self, rot: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
-                 original_len: float = 4096, beta_fast: float = 32.0, beta_slow: float = 1.0, device=None):
+                 original_len: float = 4096, beta_fast: float = 32.0, beta_slow: float = 1.0, device=None, amp: float | None = None):
         import torch
         steps, self.amp = comet_rope_steps(rot, base, scaling, factor, original_len, beta_fast, beta_slow)
+        if amp is not None:
+            self.amp = C.c_float(amp).value
+            if not abs(self.amp) < float("inf"):
+                raise ValueError(f"amp: a number of float32 expected, got {amp}")
         self.rot, self.interleaved = int(rot), bool(interleaved)
         self.steps = torch.tensor(steps, dtype=torch.int64).to(torch.device("cuda", torch.cuda.current_device()) if device is None else device)
         self.device_index = self.steps.get_device()

@@ -92,3 +92,12 @@ def test_rotation_refuses_what_asks_for_a_gradient(comet):  # noqa: F811
             comet.comet_rope(torch.zeros(2, 2, 64, requires_grad=not kw), rope, **kw)
     with torch.no_grad(), pytest.raises(ValueError):                                      # (a host tensor)
         comet.comet_rope(torch.zeros(2, 2, 64, requires_grad=True), rope)
+
+
+def test_amplitude_of_a_rotation(comet):  # noqa: F811
+    how = dict(scaling="parts", factor=8.0, original_len=8192, beta_fast=4.0, device="cpu")
+    natural, given = comet.Rope(128, **how), comet.Rope(128, amp=1.0, **how)
+    assert natural.amp > 1.2 and given.amp == 1.0 and given._plan.amp == 1.0 and given.steps.equal(natural.steps)
+    for bad in (float("nan"), float("inf"), -float("inf"), 1e39):
+        with pytest.raises(ValueError):
+            comet.Rope(128, amp=bad, device="cpu")

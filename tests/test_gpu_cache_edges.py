@@ -218,3 +218,20 @@ def test_gradients_are_not_lost(comet):  # noqa: F811
         call()
         for graph in open_graphs:
             assert next(graph, None) is None
+
+
+# ---- a rotation with an amplitude of its own -----------------------------------------------------------------------
+
+
+def test_rope_amplitude(comet):  # noqa: F811
+    """Frequencies scaled by parts, values kept as large as they are (or made as large as is asked for)."""
+    g = gen(1)
+    x = torch.randn(70, 3, 64, generator=g)
+    positions = torch.randint(0, 30000, (70,), generator=g, dtype=torch.int32)
+    how = dict(scaling="parts", factor=8.0, original_len=8192, beta_fast=4.0, beta_slow=1.0)
+    y, tol = rope_bound(x, positions, 64, False, how)
+    _, natural = ref.frequencies(64, **how)
+    for amp in (1.0, 0.25, -2.0, natural):
+        got = comet.comet_rope(x.cuda(), comet.Rope(64, amp=amp, **how), positions.cuda())
+        assert ((got.cpu().double() - y * (amp / natural)).abs() <= tol * abs(amp / natural) + U32 * y.abs() * abs(amp)).all()
+    assert comet.Rope(64, **how).amp == pytest.approx(natural, rel=2.0 ** -24)

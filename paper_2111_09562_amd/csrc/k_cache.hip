@@ -1,6 +1,7 @@
 // Keys and values into the compressed cache and out of it again.  Bound by HBM for prompts, by a chain of memory round trips for single tokens.
-// 18792 tokens, 8 + 8 heads of 128, bf16: in 37 us (3.1 TB/s; 31 without the rotation), with 32 heads of queries 100 us (4.2 TB/s), out 21 us
-// (5.6 TB/s).  64 single tokens: in 7.5 us, 11.5 if all of them complete a block, out 3.5.
+// 18792 tokens, 8 + 8 heads of 128, bf16: in 38 us (3.0 TB/s; 34 without the rotation), with 32 heads of queries 101 us (4.2 TB/s), out 20.5 us
+// (5.6 TB/s; behind the append of the same tokens, whose writes are still on their way, 30).  64 single tokens: in 7.5 us, 11.5 if all of them complete a
+// block, out 3.5.
 #include <type_traits>
 
 #include "comet_cache.h"
@@ -97,7 +98,7 @@ __device__ inline uint32_t larger16(uint32_t a, uint32_t b) { return a > b ? a :
 //   bf16 (n below 256: 127 and 254, powers of two times 127): inv is 127 / a rounded up, so x inv is above the quotient by less than 2^-22 of it,
 //     exact at the ties of the second kind, and on the right side everywhere.
 //   fp16 (seven other n up to 2047): inv + rest is 127 / a to 2^-46 of it, and x inv + x rest, rounded once, exact at a tie.  Two more instructions a
-//     value (18792 tokens in bf16: 137 us that way, with the fetch, 131 with one).
+//     value (18792 tokens, 8 heads of 128, keys and values alone: bf16 40.3 us that way, 38.8 with one; fp16 40.3, with one 39.1).
 // (A product with the rounded reciprocal of the rounded scale sends x = a / 2, which many blocks have, to 63 or 64 as those were rounded.)  Added to
 // 1.5 * 2^23 a number of at most 127 is rounded to the nearest whole number, whose low byte is the result's.  A block with Inf or NaN has the scale NaN
 // and zeros (0 times either is a NaN whose low byte is 0: a 16-bit NaN has none of its bits there).
@@ -246,8 +247,12 @@ __device__ void compress_block(const AppendArgs &a, const Seq &s, uint32_t befor
 
 }  // namespace
 
+// Wavefronts per SIMD: four are 128 registers.  Without a bound fp16 takes 132 (18792 tokens, keys and values alone, 43.4 us instead of 40.3); bf16 stays within them by
+// itself, and single tokens lose 0.3 us of 12.8 with one.
+template <typename T> constexpr int kAppendWaves = 1;
+template <> constexpr int kAppendWaves<_Float16> = 4;
 template <typename T>
-__global__ __launch_bounds__(kCacheBlock) void k_cache_append(AppendArgs a) {
+__global__ __launch_bounds__(kCacheBlock, kAppendWaves<T>) void k_cache_append(AppendArgs a) {
     extern __shared__ __align__(16) uint16_t s_rows[];
     __shared__ uint32_t s_amax[2][kBlk];
     const uint32_t tid = threadIdx.x, unit = blockIdx.x, dim = a.c.dim, pitch = dim + 8u;

@@ -5,9 +5,12 @@
 // o = O exp2(r - m - lift) / l.  r is a second reference, near the largest x + log2 b: p, which the matrix instruction takes in float16, is
 // then at most 2^15 whatever the scales of the blocks are, and weights down to 2^-21 of the largest keep all bits float16 has, down to 2^-32 some
 // (a hundred thousand tokens of next to no weight still count).  m and r move only once something exceeds them by 2^8: O
-// is hardly ever rescaled.  The whole numbers are exact in float16, so the only rounding below 32 bits is that of p, at most
-// 2^-11 of each weight.  The query goes in as float16 times a power of two of its row, which is exact for both 16-bit types but for
-// values below 2^-38 of the row's largest.
+// is hardly ever rescaled.  The whole numbers are exact in float16.  Two roundings are below 32 bits:
+//   p, to float16: at most 2^-11 of each weight.  bf16 results are rounded to 2^-8 themselves.  For float16 results the calls of up to 64 rows multiply
+//     what the rounding leaves, too; prompts (k_attend_tile) do not, where it would make three products of two: 2048 tokens behind 30720, 16 heads of
+//     256 on one, come out with 1.4 times the error of a sum in 32 bits rounded once (2.9e-4 of the result's size, 2.1e-4).
+//   the query in bf16, to float16 times a power of two of its row: at most 2^-39 of the row's largest value, and nothing for values down to 2^-31 of
+//     that.  A query in float16 goes in as it is.
 #pragma once
 #include "comet_cache.h"
 #include "comet_scan.h"

@@ -140,13 +140,13 @@ void launch_rope(const RopeArgs &r, const Rows &x, const Rows &y, uint32_t n_tok
 }
 
 // Workgroups an attention call is cut into, about.  Few rows: 768 are resident at once for heads of 128; more than that even out sequences of
-// different lengths (64 x 400 .. 16384 tokens, 8 heads: 119 us with 768, 114 with 1280, 117 with 1536), as long as a piece keeps the keys and
-// values of 2048 / dim blocks, 128 KB: beneath that, writing and joining its result costs more (64 x 300 .. 4000 tokens, 2 heads of 256: 33 us,
-// with pieces half as long 39; 128 x 500 .. 3000 tokens, 4 heads of 64: 29 and 33).  Short sequences gain nothing (48 x 8 .. 4096 tokens, 12
-// heads of 64: 25 us with 768, 27 with 1280).  Where there are few tiles, two long sequences say (120000 tokens, 8 heads), 512 pieces take 99 us,
-// 768 take 104.
+// different lengths (64 x 400 .. 16384 tokens, 8 heads: 119 us with 768, 113 with 1280, 116 with 1536), as long as a tile is not cut that has no more than
+// 2048 / dim blocks, 128 KB of keys and values (one that has more falls into equal pieces, of 64 KB at least): beneath that, writing and joining the results costs
+// more (64 x 300 .. 4000 tokens, 2 heads of 256: 33 us, with half of that 39; 128 x 500 .. 3000 tokens, 4 heads of 64: 29 and 33).  Short
+// sequences gain nothing (48 x 8 .. 4096 tokens, 12 heads of 64: 26 us with either).  Where there are few tiles, two long sequences say (120000 tokens, 8
+// heads), 512 pieces take 97 us, 768 take 103; one short sequence is cut down to four blocks, so that its latency is shared.
 // Many rows: as many as are resident, one or two per compute unit.  Beyond that what they leave for the join costs more than shorter pieces save
-// (prompts of 500 to 2000 tokens, 8 heads: 117 us with 512, 153 with 768).
+// (prompts of 500 to 2000 tokens, 8 heads: 107 us with 512, 106 with 256, 185 with 768).
 constexpr uint32_t kAttendPieces = 1280, kAttendPiecesLong = 512, kAttendTilePieces = 256;
 struct AttendPlan {
     uint32_t pieces, grid, slots, tiles, tile_shift, min_blocks;
@@ -159,7 +159,7 @@ bool plan_attend(comet_cache_shape s, uint32_t n_seqs, uint32_t n_tokens, uint32
     if (rows > kMaxRows) return false;
     p->wide = rows > 64ull * n_seqs;
     // Tiles of 256 rows for heads of up to 64, of 128 for those beyond 128 (what fits the registers); between, 256 rows once prompts are long:
-    // 8 x 4 heads of 128, prompts of 500 to 4096 tokens 137 us (128 rows: 123), 4096 tokens behind 28672 2.10 ms (2.26).
+    // 8 x 4 heads of 128, prompts of 500 to 2000 tokens 126 us (128 rows: 106), 4096 tokens behind 28672 2.14 ms (2.32).
     p->two = s.dim <= 64u || (s.dim <= 128u && n_tokens / 4096u >= n_seqs);
     p->few = rows <= 16ull * n_seqs;
     p->tile_shift = p->few ? 4u : !p->wide ? 5u : p->two ? 8u : 7u;

@@ -5,10 +5,10 @@ namespace comet {
 
 // Few rows: a wavefront holds 32 rows (queries of one key/value head, its group's heads side by side) and goes through every fourth
 // block of its workgroup's piece straight from memory into the operands of the matrix instruction, with no LDS and no barrier
-// in the loop.  Bound by HBM and the conversion to float16 together (64 sequences of 400 to 16384 tokens, 8 heads of 128, 32 rows each: 155 us with the
-// join, 3.5 TB/s).
-// EXACT: what rounding the weights to float16 leaves is multiplied as well, for results in float16, as in k_attend_few (the same sequences
-// 161 us, 156 without; 48 sequences of up to 4096 tokens, 12 heads of 64, 20 rows each 39 us and 37).
+// in the loop.  Bound by HBM and the conversion to float16 together (64 sequences of 400 to 16384 tokens, 8 heads of 128, 32 rows each: 118 us,
+// 4.5 TB/s).
+// EXACT: what rounding the weights to float16 leaves is multiplied as well, for results in float16, as in k_attend_few (with the join,
+// the same sequences 161 us, 156 without; 48 sequences of up to 4096 tokens, 12 heads of 64, 20 rows each 39 us and 37).
 // grid: heads * pieces workgroups of kAttendBlock threads, the heads of a piece side by side
 template <int NC, bool EXACT>
 __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(AttendArgs a) {
@@ -183,8 +183,8 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 4 ? 2 : 1) void k_attend(Attend
     }
 }
 
-// Fewer still: the same with tiles of 16 rows, half the registers and so twice the wavefronts and loads in flight.  Bound by HBM: the same sequences
-// 109 us (4.8 TB/s), two of 120000 tokens 91 us (5.4 TB/s; a large copy reaches 5.1); one of 701 tokens 7.6 us, a chain of memory round trips.
+// Fewer still: the same with tiles of 16 rows, half the registers and so twice the wavefronts and loads in flight.  Bound by HBM: the same sequences,
+// 4 rows each, 106 us (5.0 TB/s), two of 120000 tokens 91 us (5.4 TB/s; a large copy reaches 5.1); one of 701 tokens 7.5 us, a chain of memory round trips.
 // EXACT: what rounding the weights to float16 leaves is multiplied as well, for results in float16 (whose own rounding is no larger: together 1.45 times
 // the error of one; the second product hides behind the loads).
 template <int NC, bool EXACT>
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(kAttendBlock, NC <= 3 ? 4 : NC <= 5 ? 3 : 2) void k
 }
 
 // Joins the pieces of a row: a workgroup per row, its wavefronts (and the parts of one that a row does not fill) take the pieces in turn; their
-// sums are added in a fixed order.  3.8 us for one sequence, 6.3 for 64.  grid: (heads * tiles, rows at a time)
+// sums are added in a fixed order.  3.7 us for one sequence, 5.7 for 64, 32 if those have 32 rows each.  grid: (heads * tiles, rows at a time)
 __global__ __launch_bounds__(kAttendBlock) void k_attend_join(AttendArgs a) {
     __shared__ __align__(16) float s_o[kAttendBlock][4];
     const uint32_t tid = threadIdx.x, lane = (uint32_t)lane_id(), dim = a.c.dim;

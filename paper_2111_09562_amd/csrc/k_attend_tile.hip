@@ -24,9 +24,9 @@ __device__ inline void interleave(half8 *p, float &l) {
 //   A's weights of block j with  O_B += V(j-1) p_B  and  s_B = K(j) q_B;   B's weights with  O_A += V(j) p_A  and  s_A = K(j+1) q_A.
 // The operands stay in registers for both tiles, which halves what is read from LDS.  One tile per wavefront (RT = 1): the next block's s beside the weights,
 // then the values; the operands of the block after that are read meanwhile.
-// 8 x 4 heads of 128, 4096 tokens behind 28672: RT = 2 2.08 ms (992 TFLOP/s; products and weights one after another 797), RT = 1 2.26 ms; prompts of 582 to 1966
-// tokens: RT = 1 113 us, RT = 2 137 us.  16 heads of 256 on one of keys, 2048 tokens behind 30720: 1.16 ms, 920 TFLOP/s (8192^3 products of the
-// library: 1220 .. 1270).  Heads of 64, 4096 behind 28672: 705 TFLOP/s, the exponentials.
+// 8 x 4 heads of 128, 4096 tokens behind 28672: RT = 2 2.12 ms (970 TFLOP/s; 797 when products and weights came one after another), RT = 1 2.32 ms; prompts of 582
+// to 1966 tokens: RT = 1 103 us, with the join 106, RT = 2 126.  16 heads of 256 on one of keys, 2048 tokens behind 30720: 1.18 ms, 905 TFLOP/s (8192^3 products
+// of the library: 1220 .. 1270).  Heads of 64, 4096 behind 28672: 710 TFLOP/s, the exponentials.
 template <int NC, int RT>
 __global__ __launch_bounds__(kAttendBlock, tile_pairs(NC, RT) ? 2 : 1) void k_attend_tile(AttendArgs a) {
     constexpr uint32_t dim = 32u * NC, rows_wave = 32u * RT, rows_wg = 4u * rows_wave;

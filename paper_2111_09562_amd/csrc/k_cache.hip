@@ -1,7 +1,7 @@
 // Keys and values into the compressed cache and out of it again.  Bound by HBM for prompts, by a chain of memory round trips for single tokens.
 // 18792 tokens, 8 + 8 heads of 128, bf16: in 38 us (3.0 TB/s; 34 without the rotation), with 32 heads of queries 101 us (4.2 TB/s), out 20.5 us
-// (5.6 TB/s; behind the append of the same tokens, whose writes are still on their way, 30).  64 single tokens: in 7.5 us, 11.5 if all of them complete a
-// block, out 3.5.
+// (5.6 TB/s; behind the append of the same tokens, whose writes are still on their way, 30).  64 single tokens: in 7.8 us, 12.7 if all of them complete a
+// block, out 3.7.
 #include <type_traits>
 
 #include "comet_cache.h"
@@ -58,7 +58,8 @@ __device__ void load_block(const AppendArgs &a, const Seq &s, uint32_t before, u
     const uint16_t *kr = reinterpret_cast<const uint16_t *>(half), *vr = kr + 32u * dim;
     const float *e = reinterpret_cast<const float *>(half + 128ull * dim);
     // A round's loads, eight values of a key and four tokens of two values, wait for memory together (larger rounds cost a wavefront per SIMD:
-    // 64 tokens that all complete a block 11.5 us, 10.9 with rounds twice that, 12.7 one load at a time; 18792 tokens 136, 143 and 136 with the fetch).
+    // when they were chosen, 64 tokens that all complete a block took 11.5 us, 10.9 with rounds twice that, 12.7 one load at a time; 18792 tokens 7 us more
+    // with the large rounds).
     const uint32_t n_k = r0 * (dim / 8u), quad = token_at(4u * (threadIdx.x % 8u));           // (r0 <= 31 tokens of before)
     const f32x4 ve = *reinterpret_cast<const f32x4 *>(e + 32u + quad);
     for (uint32_t k0 = threadIdx.x, v0 = threadIdx.x; v0 < 8u * dim; k0 += kCacheBlock, v0 += 2u * kCacheBlock) {
@@ -83,8 +84,9 @@ __device__ void load_block(const AppendArgs &a, const Seq &s, uint32_t before, u
     }
 }
 
-// Power of two by which a token's values are divided on their way into float16: the largest then lies in [2^14, 2^15),
-// and only what is 2^-39 of it and less loses bits.
+// Power of two by which a token's values are divided on their way into float16: the largest then lies in [2^14, 2^15), and float16 steps there end at
+// 2^-24.  So a value is off by at most 2^-39 of the token's largest, and a bf16 value by nothing down to 2^-31 of that.  (A block's values in
+// 8 bits do not notice: what was rounded here is 0 there.)
 __device__ inline float token_scale(float amax) {
     uint32_t e = __float_as_uint(amax) >> 23;
     if (e < 15u) e = 15u;

@@ -1,7 +1,7 @@
 // Rotary positions: every pair of a head's rotated part is turned by its position times the pair's step.  The gradient is the
 // same rotation the other way, so the backward pass needs the positions and nothing of the forward pass.
 // Bound by HBM: 16 bytes a lane and access, neighbouring lanes on neighbouring chunks of a head; a chunk's sines are computed once for up to eight
-// heads.  16384 x 32 x 128 bf16: 55 us, 4.9 TB/s; 4099 x 20 x 96 fp32, 64 of them side by side: 12.2 us, 5.2 TB/s; 16 tokens: 3.5 us, a launch.
+// heads.  16384 x 32 x 128 bf16: 56 us, 4.8 TB/s; 4099 x 20 x 96 fp32, 64 of them side by side: 12.2 us, 5.2 TB/s; 16 tokens: 3.5 us, a launch.
 #include "comet_cache.h"
 
 namespace comet {
